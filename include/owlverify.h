@@ -236,6 +236,80 @@ int owl_kv_commit(owl_ctx* ctx, const owl_dims* dims, void* k_cache, void* v_cac
                   const int32_t* block_table, int32_t* ctx_lens, const int32_t* node_offsets,
                   const int32_t* accept_len, const int32_t* accept_path, void* stream);
 
+/* Element types of the calls that take one (`dtype`). */
+#define OWL_DTYPE_BF16 0
+#define OWL_DTYPE_F16 1
+#define OWL_DTYPE_F32 2
+
+/*
+ * The step before owl_verify_attn: queries and keys of the appended tokens get their rotary positions (Section 3.2.2 "Decode
+ * Stage": the position ids are manipulated along with the mask), keys and values go to the paged cache.
+ * Token i of sequence b (packed row t = node_offsets[b] + i) goes to logical position ctx_lens[b] + i, its angle is that of
+ * positions[t]:
+ *   x'[j] = x[j] cos[j] - x[j+64] sin[j],  x'[j+64] = x[j+64] cos[j] + x[j] sin[j],  j = 0 .. 63,
+ * in fp32, each product and sum rounded by itself, then rounded once to the output's type.
+ *
+ * dtype: OWL_DTYPE_BF16 or OWL_DTYPE_F16, that of q, k, v, q_out and the caches.  k, v [total_nodes, Hkv, 128], q [total_nodes,
+ * Hq, 128]; a token's heads are contiguous, from one token to the next it is *_stride elements (a multiple of 8), so the three
+ * may be parts of one projection's output.  q may be NULL (then num_q_heads and q_out are not looked at); q_out [total_nodes,
+ * Hq, 128] contiguous receives the turned queries, and may be q itself where that is contiguous.  positions int32
+ * [total_nodes], NULL for ctx_lens[b] + i (a chain, a prompt); rope fp32 [rope_rows, 128], row m the 64 cosines and 64 sines of
+ * position m (scaled as the model wants them); NULL, with rope_rows 0: nothing is turned.  block_table, ctx_lens, node_offsets
+ * as for owl_verify_attn, but dims->total_nodes counts tokens of any number per sequence, none included (a prompt's too:
+ * max_nodes is not looked at).  ctx_lens is read only: drafts are committed by owl_kv_commit, a prompt by adding its
+ * length.  All pointers but node_offsets and the int32 arrays 16-byte aligned.  Slots other than the tokens' own are left as they
+ * are.  Asynchronous on `stream`.
+ * Device-detected: offsets that do not describe the rows set OWL_ERR_BAD_TREE; a sequence that does not fit its row of the
+ * block_table is left out as a whole, a token on a page out of range is not written to the cache and one whose position the table lacks not
+ * at all (OWL_ERR_BAD_PAGE).
+ */
+int owl_kv_append(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void* q, int64_t q_stride, const void* k,
+                  int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions, const float* rope,
+                  int32_t rope_rows, void* q_out, void* k_cache, void* v_cache, const int32_t* block_table,
+                  const int32_t* ctx_lens, const int32_t* node_offsets, void* stream);
+
+/*
+ * The 8-bit cache.  k_cache, v_cache [num_pages, Hkv, page_size, 128] of e4m3 (1 byte); page_exp int8 [num_pages, Hkv, 2]: the
+ * exponents of a page's K and V of one head, the block's elements standing for e4m3 * 2^exponent.  Exponents lie in -24 .. 7
+ * (one outside reads as the nearer end).  A block's exponent is the smallest there for which its largest magnitude is at most
+ * 448 * 2^exponent; magnitudes above 448 * 2^7 = 57344 saturate, a NaN stays one.
+ *
+ * owl_kv_append_fp8 is owl_kv_append into such a cache (dtype is that of q, k, v and q_out).  A page whose first slot receives a
+ * token takes the exponent that its new rows need; another page the larger of its own and that, and if it grows the rows of the
+ * context on the page (those before ctx_lens[b]) are re-encoded.  A page that receives tokens must belong to one sequence only.
+ */
+int owl_kv_append_fp8(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void* q, int64_t q_stride, const void* k,
+                      int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions, const float* rope,
+                      int32_t rope_rows, void* q_out, void* k_cache, void* v_cache, int8_t* page_exp,
+                      const int32_t* block_table, const int32_t* ctx_lens, const int32_t* node_offsets, void* stream);
+
+/*
+ * owl_kv_commit in the 8-bit cache.  A page that rows move to takes the larger of its exponent and what those rows need; if it
+ * grows, the rows that stay on it (the context's and accepted ones in place already) are re-encoded.  Other slots keep their
+ * bytes.
+ */
+int owl_kv_commit_fp8(owl_ctx* ctx, const owl_dims* dims, void* k_cache, void* v_cache, int8_t* page_exp,
+                      const int32_t* block_table, int32_t* ctx_lens, const int32_t* node_offsets,
+                      const int32_t* accept_len, const int32_t* accept_path, void* stream);
+
+/*
+ * Log probabilities of given tokens, with entropy and the most likely alternatives, from the rows that owl_tree_accept reads:
+ *   lse[r] = ln sum_v exp(logits[r, v]),   entropy[r] = -sum_v p ln p with p = exp(logits[r, v] - lse[r]),
+ *   top_ids[r, 0..top), top_logprobs[r, 0..top): the tokens of greatest logits, the lower token first among equals,
+ *   logprob[n] = logits[row(n), tokens[n]] - lse[row(n)].
+ * With tree_parent, row(n) is the row of node n's parent (as in the acceptance: what the parent's row says of the drafted
+ * token), and a root scores 0; with tree_parent NULL, row(n) = n.  A negative token ([SPEC], none) scores 0, one beyond the
+ * vocabulary -inf.  logits [N, V] row-major of `dtype` (fp32, bf16 or fp16; sums in fp32), tokens int32 [N]; outputs fp32 [N],
+ * int32 / fp32 [N, top], top 0..32.  logprob (and then tokens), entropy, lse and one of the top_* may be NULL; with top 0 both
+ * top_* are.  NaN and -inf logits have probability 0 and are no alternatives (missing ones: id -1, -inf).  A row
+ * without anything else has lse -inf, entropy 0 and every log probability -inf; a row with +inf has lse +inf, entropy NaN
+ * and log probability -inf for finite logits, NaN for infinite ones.  A malformed offset or parent sets
+ * OWL_ERR_BAD_TREE and leaves that node's logprob unwritten.  Asynchronous on `stream`; results do not depend on timing.
+ */
+int owl_token_logprobs(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void* logits, const int32_t* tokens,
+                       const int32_t* node_offsets, const int32_t* tree_parent, int32_t top, float* logprob, float* entropy,
+                       float* lse, int32_t* top_ids, float* top_logprobs, void* stream);
+
 /*
  * Acceptance straight from the verifier's last hidden states (Introduction: the target model's forward over the
  * drafted tokens ends in logits, from which the accepted tokens follow): logits[n, :] = hidden[n, :] . weight^T is

@@ -298,3 +298,8 @@ def lstm_cell(h_bits, emb_bits, w_bits, z, alpha: float, ln_c=(None, None), ln_z
     z_next = np.asarray(z, dtype=np.float64) * gf + sc
     h_next = _layer_norm_gelu(z_next, ln_z[0], ln_z[1], eps) * go
     return h_next, z_next
+
+
+# ----------------------------------------------------------------------------- append, 8-bit cache, log probabilities
+from .cache8 import (E4M3, block_exponent, cache8_values, e4m3_encode, kv_append, kv_append_fp8, kv_commit_fp8, rotate,  # noqa: E402,F401
+                     token_logprobs)

@@ -167,6 +167,38 @@ class OwlContext:
         rc = _native.kv_commit(self._handle, self._dev, dims, k_cache, v_cache, block_table, ctx_lens, node_offsets, accept_len, accept_path)
         return self._done(rc, check, "owl_kv_commit")
 
+    def owl_kv_append(self, dims: OwlDims, q, k, v, positions, rope, q_out, k_cache, v_cache, block_table, ctx_lens, node_offsets,
+                      check: bool = True) -> int:
+        """``q``, ``k``, ``v``: [tokens, heads, 128], tokens may be strided (slices of a fused projection); the element type is
+        ``k``'s.  ``rope``: [positions, 128] cosines and sines, or None."""
+        rc = _native.kv_append(self._handle, self._dev, dims, q, k, v, positions, rope, q_out, k_cache, v_cache, block_table, ctx_lens, node_offsets)
+        return self._done(rc, check, "owl_kv_append")
+
+    def owl_kv_append_fp8(self, dims: OwlDims, q, k, v, positions, rope, q_out, k_cache, v_cache, page_exp, block_table, ctx_lens, node_offsets,
+                          check: bool = True) -> int:
+        """As ``owl_kv_append`` into float8_e4m3fn caches with int8 ``page_exp`` [num_pages, Hkv, 2]."""
+        rc = _native.kv_append_fp8(self._handle, self._dev, dims, q, k, v, positions, rope, q_out, k_cache, v_cache, page_exp, block_table, ctx_lens,
+                                   node_offsets)
+        return self._done(rc, check, "owl_kv_append_fp8")
+
+    def owl_kv_commit_fp8(self, dims: OwlDims, k_cache, v_cache, page_exp, block_table, ctx_lens, node_offsets, accept_len, accept_path,
+                          check: bool = True) -> int:
+        rc = _native.kv_commit_fp8(self._handle, self._dev, dims, k_cache, v_cache, page_exp, block_table, ctx_lens, node_offsets, accept_len, accept_path)
+        return self._done(rc, check, "owl_kv_commit_fp8")
+
+    def owl_token_logprobs(self, dims: OwlDims, logits, tokens, node_offsets, tree_parent, logprob=None, entropy=None, lse=None, top_ids=None,
+                           top_logprobs=None, check: bool = True) -> int:
+        """The number of alternatives is the last dimension of ``top_ids`` / ``top_logprobs`` (None or an empty one: none)."""
+        tops = [t for t in (top_ids, top_logprobs) if t is not None]
+        top = int(tops[0].shape[-1]) if tops else 0
+        if any(int(t.shape[-1]) != top for t in tops):
+            raise TypeError("top_ids and top_logprobs differ in their last dimension")
+        if top == 0:
+            top_ids = top_logprobs = None
+        rc = _native.token_logprobs(self._handle, self._dev, dims, top, logits, tokens, node_offsets, tree_parent, logprob, entropy, lse, top_ids,
+                                    top_logprobs)
+        return self._done(rc, check, "owl_token_logprobs")
+
     def owl_lm_head_accept(self, dims: OwlDims, hidden, weight, draft_tokens, node_offsets, tree_parent, accept_len, accept_path,
                            bonus_token, node_argmax=None, check: bool = True) -> int:
         rc = _native.lm_head_accept(self._handle, self._dev, dims, int((weight if hidden is None else hidden).shape[-1]), hidden, weight,

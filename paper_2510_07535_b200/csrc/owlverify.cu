@@ -13,6 +13,9 @@
 #include "accept.cuh"
 #include "combine.cuh"
 #include "gemm_umma.cuh"
+#include "kv_append.cuh"
+#include "kv_commit_fp8.cuh"
+#include "logprobs.cuh"
 #include "owl_common.cuh"
 #include "spec_loop.cuh"
 #include "verify_attn_umma.cuh"
@@ -36,6 +39,10 @@ struct owl_ctx {
     unsigned long long* part_keys = nullptr;
     unsigned long long* lm_keys = nullptr;      // KeySets: two sets of one arg-max key per row, then the call numbers
     long long part_keys_len = 0;
+    ScorePartial* score_part = nullptr;         // owl_token_logprobs: sums and lists of its (row, chunk) items, the rows' sums
+    unsigned long long* score_keys = nullptr;
+    float2* score_rows = nullptr;
+    long long score_len = 0;                    // items
     // tensor maps over the callers' K and V caches: a few most recently used (cache pointers, geometry) pairs
     // are kept, so that a caller rotating over several caches does not pay two encodes per call
     EncodeTiledFn encode = nullptr;
@@ -205,6 +212,40 @@ int launch_gemm(owl_ctx* ctx, const void* a, const void* b, int M, int N, int K,
     return OWL_OK;
 }
 
+// Launch of a commit kernel: a cluster of CTAs per sequence.
+template <typename Params>
+int launch_commit(owl_ctx* ctx, void (*kernel)(Params), const Params& p, const CommitParams& c, void* stream, const char* what) {
+    const unsigned cluster = c.num_kv_heads < kCommitMaxCluster ? (unsigned)c.num_kv_heads : (unsigned)kCommitMaxCluster;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(cluster, (unsigned)c.batch);
+    cfg.blockDim = dim3(kCommitThreads);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cudaLaunchKernelEx(&cfg, kernel, p);
+    ++ctx->launches;
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(ctx, e, what);
+    return OWL_OK;
+}
+
+// One turn of owl_token_logprobs: the scan of the rows [p.row0, p.row0 + p.rows) and their merge.
+template <typename T>
+void launch_score(owl_ctx* ctx, const ScoreParams& p, cudaStream_t stream) {
+    const long long items = (long long)p.rows * p.chunks, most = (long long)ctx->sm_count * kScoreCtasPerSm;
+    const long long ctas = (items + kScoreWarps - 1) / kScoreWarps;
+    launch_dependent(p.top > 0 ? logprob_scan_kernel<T, true> : logprob_scan_kernel<T, false>, dim3((unsigned)(ctas < most ? ctas : most)),
+                     dim3(kScoreWarps * 32), stream, p);
+    launch_dependent(logprob_merge_kernel<T>, dim3((unsigned)p.rows), dim3(kScoreWarps * 32), stream, p);
+    ctx->launches += 2;
+}
+
 }  // namespace
 
 extern "C" {
@@ -273,6 +314,10 @@ int owl_create(owl_ctx** out, int device, const owl_dims* max_dims) {
         const size_t lm_bytes = (2 * (size_t)max_dims->total_nodes + 1) * sizeof(unsigned long long);
         alloc((void**)&ctx->lm_keys, lm_bytes);
         if (ok) ok = cudaMemset(ctx->lm_keys, 0, lm_bytes) == cudaSuccess;
+        ctx->score_len = score_room(max_dims->total_nodes, max_dims->vocab, ctx->sm_count);
+        alloc((void**)&ctx->score_part, (size_t)ctx->score_len * sizeof(ScorePartial));
+        alloc((void**)&ctx->score_keys, (size_t)ctx->score_len * kMaxTop * sizeof(unsigned long long));
+        alloc((void**)&ctx->score_rows, (size_t)max_dims->total_nodes * sizeof(float2));
     }
     if (ok) {
         ok = cudaMemset(ctx->status, 0, sizeof(int32_t)) == cudaSuccess;
@@ -316,6 +361,9 @@ int owl_destroy(owl_ctx* ctx) {
     cudaFree(ctx->sched_header);
     cudaFree(ctx->part_keys);
     cudaFree(ctx->lm_keys);
+    cudaFree(ctx->score_part);
+    cudaFree(ctx->score_keys);
+    cudaFree(ctx->score_rows);
     for (auto& s : ctx->stg) cudaFree(s.p);
     for (auto& ev : ctx->ev)
         if (ev) cudaEventDestroy(ev);
@@ -602,9 +650,9 @@ int owl_howl_route(int32_t batch, const float* score, float c, uint8_t* lastwasl
     return OWL_OK;
 }
 
-int owl_kv_commit(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v_cache, const int32_t* block_table,
-                  int32_t* ctx_lens, const int32_t* node_offsets, const int32_t* accept_len, const int32_t* accept_path,
-                  void* stream_) {
+// Argument checks of the commit and its kernel parameters.
+static int commit_params(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v_cache, const int32_t* block_table, int32_t* ctx_lens,
+                         const int32_t* node_offsets, const int32_t* accept_len, const int32_t* accept_path, CommitParams& p) {
     if (!ctx) return OWL_ERR_INVALID_ARG;
     int rc = check_dims(d, false, false);
     if (rc != OWL_OK) return rc;
@@ -614,9 +662,7 @@ int owl_kv_commit(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v_cache,
         return OWL_ERR_UNSUPPORTED;
     if (!k_cache || !v_cache || !block_table || !ctx_lens || !accept_len || !accept_path) return OWL_ERR_INVALID_ARG;
     if (!node_offsets && d->total_nodes % d->batch != 0) return OWL_ERR_INVALID_ARG;
-    DeviceGuard guard(ctx->device);
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    CommitParams p{};
+    p = CommitParams{};
     p.k_cache = static_cast<__nv_bfloat16*>(k_cache); p.v_cache = static_cast<__nv_bfloat16*>(v_cache);
     p.block_table = block_table; p.ctx_lens = ctx_lens; p.node_offsets = node_offsets;
     p.accept_len = accept_len; p.accept_path = accept_path; p.status = ctx->status;
@@ -624,23 +670,135 @@ int owl_kv_commit(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v_cache,
     p.max_nodes = d->max_nodes; p.num_kv_heads = d->num_kv_heads;
     p.page_size = d->page_size; p.page_shift = log2_exact(d->page_size);
     p.max_pages_per_seq = d->max_pages_per_seq; p.num_pages = d->num_pages; p.path_stride = d->path_stride;
-    const unsigned cluster = d->num_kv_heads < kCommitMaxCluster ? (unsigned)d->num_kv_heads : (unsigned)kCommitMaxCluster;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(cluster, (unsigned)d->batch);
-    cfg.blockDim = dim3(kCommitThreads);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    cudaLaunchKernelEx(&cfg, kv_commit_kernel, p);
+    return OWL_OK;
+}
+int owl_kv_commit(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v_cache, const int32_t* block_table,
+                  int32_t* ctx_lens, const int32_t* node_offsets, const int32_t* accept_len, const int32_t* accept_path,
+                  void* stream_) {
+    CommitParams p;
+    const int rc = commit_params(ctx, d, k_cache, v_cache, block_table, ctx_lens, node_offsets, accept_len, accept_path, p);
+    if (rc != OWL_OK) return rc;
+    DeviceGuard guard(ctx->device);
+    return launch_commit(ctx, kv_commit_kernel, p, p, stream_, "owl_kv_commit launch");
+}
+
+int owl_kv_commit_fp8(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v_cache, int8_t* page_exp, const int32_t* block_table,
+                      int32_t* ctx_lens, const int32_t* node_offsets, const int32_t* accept_len, const int32_t* accept_path,
+                      void* stream_) {
+    CommitFp8Params p;
+    const int rc = commit_params(ctx, d, k_cache, v_cache, block_table, ctx_lens, node_offsets, accept_len, accept_path, p.base);
+    if (rc != OWL_OK) return rc;
+    if (!page_exp) return OWL_ERR_INVALID_ARG;
+    p.page_exp = page_exp;
+    DeviceGuard guard(ctx->device);
+    return launch_commit(ctx, kv_commit_fp8_kernel, p, p.base, stream_, "owl_kv_commit_fp8 launch");
+}
+
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The append in all its forms: `page_exp` non-null for the 8-bit cache.
+static int kv_append_impl(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                          const void* v, int64_t v_stride, const int32_t* positions, const float* rope, int32_t rope_rows, void* q_out,
+                          void* k_cache, void* v_cache, int8_t* page_exp, bool fp8, const int32_t* block_table, const int32_t* ctx_lens,
+                          const int32_t* node_offsets, void* stream_) {
+    if (!ctx || !d) return OWL_ERR_INVALID_ARG;
+    // (a prompt has more tokens than a draft may have nodes: total_nodes counts tokens here, max_nodes is not looked at)
+    if (d->batch < 1 || d->total_nodes < 1 || d->num_kv_heads < 1 || d->max_pages_per_seq < 1 || d->num_pages < 1) return OWL_ERR_INVALID_ARG;
+    if (q && (d->num_q_heads < 1 || !q_out)) return OWL_ERR_INVALID_ARG;
+    if (dtype != OWL_DTYPE_BF16 && dtype != OWL_DTYPE_F16) return OWL_ERR_INVALID_ARG;
+    if (d->batch > kMaxBatch || d->num_kv_heads > 128 || d->head_dim != kHeadDim || (q && d->num_q_heads > 65535 - 128) ||
+        !(d->page_size == 16 || d->page_size == 32 || d->page_size == 64 || d->page_size == 128))
+        return OWL_ERR_UNSUPPORTED;
+    if (!k || !v || !k_cache || !v_cache || (fp8 && !page_exp) || !block_table || !ctx_lens) return OWL_ERR_INVALID_ARG;
+    if (!node_offsets && d->total_nodes % d->batch != 0) return OWL_ERR_INVALID_ARG;
+    if (rope ? rope_rows < 1 : rope_rows != 0) return OWL_ERR_INVALID_ARG;
+    // rows are read and written in 16-byte pieces
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(rope) || !aligned16(q) || !aligned16(q_out) ||
+        k_stride < 0 || v_stride < 0 || q_stride < 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || q_stride % 8 != 0)
+        return OWL_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    AppendParams p{};
+    p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v);
+    p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride;
+    p.positions = positions; p.rope = rope; p.rope_rows = rope_rows;
+    p.q_out = static_cast<__nv_bfloat16*>(q_out);
+    p.k_cache = k_cache; p.v_cache = v_cache; p.page_exp = page_exp;
+    p.block_table = block_table; p.ctx_lens = ctx_lens; p.node_offsets = node_offsets; p.status = ctx->status;
+    p.batch = d->batch; p.total_nodes = d->total_nodes; p.nodes_uniform = d->total_nodes / d->batch;
+    p.num_q_heads = d->num_q_heads; p.num_kv_heads = d->num_kv_heads;
+    p.page_size = d->page_size; p.page_shift = log2_exact(d->page_size);
+    p.max_pages_per_seq = d->max_pages_per_seq; p.num_pages = d->num_pages;
+    const long long items = (d->total_nodes >> p.page_shift) + 2ll * d->batch;
+    p.kv_heads_per_group = append_heads_per_group(items, d->num_kv_heads, d->page_size, ctx->sm_count);
+    p.kv_groups = (d->num_kv_heads + p.kv_heads_per_group - 1) / p.kv_heads_per_group;
+    int q_groups = 0;
+    if (q) {
+        p.q_heads_per_group = append_heads_per_group(items, d->num_q_heads, d->page_size, ctx->sm_count);
+        q_groups = (d->num_q_heads + p.q_heads_per_group - 1) / p.q_heads_per_group;
+    }
+    const bool f16 = dtype == OWL_DTYPE_F16;
+    auto* kernel = fp8 ? (f16 ? kv_append_kernel<true, true> : kv_append_kernel<false, true>)
+                       : (f16 ? kv_append_kernel<true, false> : kv_append_kernel<false, false>);
+    launch_dependent(kernel, dim3((unsigned)items, (unsigned)(p.kv_groups + q_groups)), dim3(8u * (unsigned)d->page_size),
+                     static_cast<cudaStream_t>(stream_), p);
     ++ctx->launches;
     cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(ctx, e, "owl_kv_commit launch");
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "owl_kv_append launch");
+    return OWL_OK;
+}
+
+int owl_kv_append(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                  const void* v, int64_t v_stride, const int32_t* positions, const float* rope, int32_t rope_rows, void* q_out,
+                  void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* ctx_lens, const int32_t* node_offsets,
+                  void* stream_) {
+    return kv_append_impl(ctx, d, dtype, q, q_stride, k, k_stride, v, v_stride, positions, rope, rope_rows, q_out, k_cache, v_cache, nullptr,
+                          false, block_table, ctx_lens, node_offsets, stream_);
+}
+
+int owl_kv_append_fp8(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                      const void* v, int64_t v_stride, const int32_t* positions, const float* rope, int32_t rope_rows, void* q_out,
+                      void* k_cache, void* v_cache, int8_t* page_exp, const int32_t* block_table, const int32_t* ctx_lens,
+                      const int32_t* node_offsets, void* stream_) {
+    return kv_append_impl(ctx, d, dtype, q, q_stride, k, k_stride, v, v_stride, positions, rope, rope_rows, q_out, k_cache, v_cache, page_exp,
+                          true, block_table, ctx_lens, node_offsets, stream_);
+}
+
+int owl_token_logprobs(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const void* logits, const int32_t* tokens, const int32_t* node_offsets,
+                       const int32_t* tree_parent, int32_t top, float* logprob, float* entropy, float* lse, int32_t* top_ids,
+                       float* top_logprobs, void* stream_) {
+    if (!ctx) return OWL_ERR_INVALID_ARG;
+    int rc = check_dims(d, false, false);
+    if (rc != OWL_OK) return rc;
+    if (d->vocab < 1 || !logits || top < 0 || (logprob && !tokens) || (top > 0) != (top_ids || top_logprobs)) return OWL_ERR_INVALID_ARG;
+    if (!logprob && !entropy && !lse && top == 0) return OWL_ERR_INVALID_ARG;
+    if (dtype != OWL_DTYPE_BF16 && dtype != OWL_DTYPE_F16 && dtype != OWL_DTYPE_F32) return OWL_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(logits) % (dtype == OWL_DTYPE_F32 ? 4 : 2)) return OWL_ERR_INVALID_ARG;
+    if (top > kMaxTop) return OWL_ERR_UNSUPPORTED;
+    if (!node_offsets && d->total_nodes % d->batch != 0) return OWL_ERR_INVALID_ARG;
+    const long long most = ctx->score_len;
+    if (!ctx->score_part || d->total_nodes > ctx->max_dims.total_nodes || ((long long)d->vocab + kScoreMaxChunk - 1) / kScoreMaxChunk > most)
+        return OWL_ERR_TOO_LARGE;
+    DeviceGuard guard(ctx->device);
+    ScoreParams p{};
+    p.logits = logits; p.tokens = tokens; p.node_offsets = node_offsets; p.tree_parent = tree_parent;
+    p.logprob = logprob; p.entropy = entropy; p.lse = lse; p.top_ids = top_ids; p.top_logprobs = top_logprobs;
+    p.part = ctx->score_part; p.part_keys = ctx->score_keys; p.status = ctx->status;
+    p.batch = d->batch; p.total_nodes = d->total_nodes; p.nodes_uniform = d->total_nodes / d->batch; p.max_nodes = d->max_nodes;
+    p.vocab = d->vocab; p.top = top;
+    p.chunk = score_chunk(d->total_nodes, d->vocab, ctx->sm_count, most);
+    p.chunks = (int32_t)(((long long)d->vocab + p.chunk - 1) / p.chunk);
+    const long long rows_at_once = most / p.chunks;
+    if (d->total_nodes > rows_at_once) p.row_sums = ctx->score_rows;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    for (long long row0 = 0; row0 < d->total_nodes; row0 += rows_at_once) {
+        p.row0 = (int32_t)row0;
+        p.rows = (int32_t)(d->total_nodes - row0 < rows_at_once ? d->total_nodes - row0 : rows_at_once);
+        if (dtype == OWL_DTYPE_F32) launch_score<float>(ctx, p, stream);
+        else if (dtype == OWL_DTYPE_F16) launch_score<__half>(ctx, p, stream);
+        else launch_score<__nv_bfloat16>(ctx, p, stream);
+    }
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "owl_token_logprobs launch");
     return OWL_OK;
 }
 

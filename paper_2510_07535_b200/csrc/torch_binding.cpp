@@ -16,7 +16,7 @@
 
 namespace {
 
-enum Type { kI32, kF32, kBf16, kF16 };
+enum Type { kI32, kF32, kBf16, kF16, kI8, kE4m3 };
 struct Spec { const char* name; Type type; };
 
 const char* type_name(Type t) {
@@ -24,6 +24,8 @@ const char* type_name(Type t) {
         case kI32: return "torch.int32";
         case kF32: return "torch.float32";
         case kBf16: return "torch.bfloat16";
+        case kI8: return "torch.int8";
+        case kE4m3: return "torch.float8_e4m3fn";
         default: return "torch.float16";
     }
 }
@@ -32,6 +34,8 @@ at::ScalarType scalar_type(Type t) {
         case kI32: return at::kInt;
         case kF32: return at::kFloat;
         case kBf16: return at::kBFloat16;
+        case kI8: return at::kChar;
+        case kE4m3: return at::kFloat8_e4m3fn;
         default: return at::kHalf;
     }
 }
@@ -212,6 +216,102 @@ OWL_CALL(lstm_cell) {
         return owl_lstm_cell(h.ctx, rows, d_in, d, p[0], p[1], p[2], alpha, f(3), f(4), f(5), f(6), eps, f(7), f(8), p[9], f(10), stream);
     });
 }
+// The element type that a call goes by: that of the tensor `o`, one of bf16, fp16 and (where `f32`) fp32.
+bool dtype_of(PyObject* o, const char* name, bool f32, Type* type, int* code) {
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a tensor", name);
+        return false;
+    }
+    const at::ScalarType t = THPVariable_Unpack(o).scalar_type();
+    if (t == at::kBFloat16) { *type = kBf16; *code = OWL_DTYPE_BF16; }
+    else if (t == at::kHalf) { *type = kF16; *code = OWL_DTYPE_F16; }
+    else if (t == at::kFloat && f32) { *type = kF32; *code = OWL_DTYPE_F32; }
+    else {
+        PyErr_Format(PyExc_TypeError, "%s: expected torch.bfloat16%s or torch.float16, got %s", name, f32 ? ", torch.float32" : "", c10::toString(t));
+        return false;
+    }
+    return true;
+}
+// A [tokens, heads, 128] tensor whose tokens may lie further apart than their heads take (part of a fused projection's output).
+bool token_rows(PyObject* o, const char* name, Type type, int heads, int tokens, int device, void** out, int64_t* stride) {
+    *out = nullptr;
+    *stride = 0;
+    if (o == Py_None) return true;
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a tensor or None", name);
+        return false;
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.scalar_type() != scalar_type(type) || !t.is_cuda() || t.get_device() != device || t.dim() != 3 || t.size(0) != tokens ||
+        t.size(1) != heads || t.size(2) != 128 || t.stride(2) != 1 || (heads > 1 && t.stride(1) != 128)) {
+        PyErr_Format(PyExc_TypeError, "%s: expected %s tensor [%d, %d, 128] on cuda:%d with contiguous heads, got %s on %s", name,
+                     type_name(type), tokens, heads, device, c10::toString(t.scalar_type()), t.device().str().c_str());
+        return false;
+    }
+    *out = t.data_ptr();
+    *stride = tokens > 1 ? t.stride(0) : 128 * (int64_t)heads;
+    return true;
+}
+// (handle, device, dims, q, k, v, positions, rope, q_out, k_cache, v_cache, [page_exp,] block_table, ctx_lens, node_offsets)
+PyObject* append_call(PyObject* const* args, Py_ssize_t nargs, bool fp8) {
+    Head h;
+    owl_dims d;
+    int dtype;
+    Type type;
+    void *q, *k, *v, *p[9];
+    int64_t qs, ks, vs;
+    if (!h.parse(args, nargs, fp8 ? 15 : 14) || !dims_of(args[2], &d) || !dtype_of(args[4], "k", false, &type, &dtype)) return nullptr;
+    if (!token_rows(args[3], "q", type, d.num_q_heads, d.total_nodes, h.device, &q, &qs) ||
+        !token_rows(args[4], "k", type, d.num_kv_heads, d.total_nodes, h.device, &k, &ks) ||
+        !token_rows(args[5], "v", type, d.num_kv_heads, d.total_nodes, h.device, &v, &vs))
+        return nullptr;
+    const Type cache = fp8 ? kE4m3 : type;
+    const Spec s16[] = {{"positions", kI32}, {"rope", kF32}, {"q_out", type}, {"k_cache", cache}, {"v_cache", cache}, {"block_table", kI32},
+                        {"ctx_lens", kI32}, {"node_offsets", kI32}};
+    const Spec s8[] = {{"positions", kI32}, {"rope", kF32}, {"q_out", type}, {"k_cache", cache}, {"v_cache", cache}, {"page_exp", kI8},
+                       {"block_table", kI32}, {"ctx_lens", kI32}, {"node_offsets", kI32}};
+    if (!tensors(args + 6, fp8 ? s8 : s16, fp8 ? 9 : 8, h.device, p)) return nullptr;
+    int rows = 0;
+    if (args[7] != Py_None) {
+        const at::Tensor& t = THPVariable_Unpack(args[7]);
+        if (t.dim() != 2 || t.size(1) != 128 || t.size(0) > 0x7fffffff) {
+            PyErr_SetString(PyExc_TypeError, "rope: expected [positions, 128]");
+            return nullptr;
+        }
+        rows = (int)t.size(0);
+    }
+    auto i = [&](int n) { return static_cast<int32_t*>(p[n]); };
+    const float* rope = static_cast<float*>(p[1]);
+    void* stream = h.stream();
+    return unlocked([&] {
+        return fp8 ? owl_kv_append_fp8(h.ctx, &d, dtype, q, qs, k, ks, v, vs, i(0), rope, rows, p[2], p[3], p[4], static_cast<int8_t*>(p[5]), i(6),
+                                       i(7), i(8), stream)
+                   : owl_kv_append(h.ctx, &d, dtype, q, qs, k, ks, v, vs, i(0), rope, rows, p[2], p[3], p[4], i(5), i(6), i(7), stream);
+    });
+}
+OWL_CALL(kv_append) { return append_call(args, nargs, false); }
+OWL_CALL(kv_append_fp8) { return append_call(args, nargs, true); }
+OWL_CALL(kv_commit_fp8) {
+    static const Spec s[] = {{"k_cache", kE4m3}, {"v_cache", kE4m3}, {"page_exp", kI8}, {"block_table", kI32}, {"ctx_lens", kI32},
+                             {"node_offsets", kI32}, {"accept_len", kI32}, {"accept_path", kI32}};
+    return pointer_call(owl_kv_commit_fp8, s, args, nargs);
+}
+// (handle, device, dims, top, logits, tokens, node_offsets, tree_parent, logprob, entropy, lse, top_ids, top_logprobs)
+OWL_CALL(token_logprobs) {
+    Head h;
+    owl_dims d;
+    int top, dtype;
+    Type type;
+    void* p[9];
+    if (!h.parse(args, nargs, 13) || !dims_of(args[2], &d) || !int_of(args[3], &top) || !dtype_of(args[4], "logits", true, &type, &dtype)) return nullptr;
+    const Spec s[] = {{"logits", type}, {"tokens", kI32}, {"node_offsets", kI32}, {"tree_parent", kI32}, {"logprob", kF32}, {"entropy", kF32},
+                      {"lse", kF32}, {"top_ids", kI32}, {"top_logprobs", kF32}};
+    if (!tensors(args + 4, s, 9, h.device, p)) return nullptr;
+    auto i = [&](int n) { return static_cast<int32_t*>(p[n]); };
+    auto f = [&](int n) { return static_cast<float*>(p[n]); };
+    void* stream = h.stream();
+    return unlocked([&] { return owl_token_logprobs(h.ctx, &d, dtype, p[0], i(1), i(2), i(3), top, f(4), f(5), f(6), i(7), f(8), stream); });
+}
 // (0, device, dims, tensors): no context
 OWL_CALL(tree_accept_static) {
     static const Spec s[] = {{"logits", kF32}, {"draft_tokens", kI32}, {"node_offsets", kI32}, {"tree_parent", kI32}, {"accept_len", kI32},
@@ -237,7 +337,8 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 #define OWL_METHOD(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {OWL_METHOD(verify_attn), OWL_METHOD(verify_attn_f16), OWL_METHOD(tree_accept), OWL_METHOD(tree_accept_spec),
                          OWL_METHOD(verify_step), OWL_METHOD(kv_commit), OWL_METHOD(prepare_spec_tree), OWL_METHOD(prepare_hybrid),
-                         OWL_METHOD(lm_head_accept), OWL_METHOD(lstm_cell), OWL_METHOD(tree_accept_static), {nullptr, nullptr, 0, nullptr}};
+                         OWL_METHOD(lm_head_accept), OWL_METHOD(lstm_cell), OWL_METHOD(tree_accept_static), OWL_METHOD(kv_append),
+                         OWL_METHOD(kv_append_fp8), OWL_METHOD(kv_commit_fp8), OWL_METHOD(token_logprobs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_owl_native", "Tensor marshalling for libowlverify", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

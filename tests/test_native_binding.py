@@ -56,3 +56,24 @@ def test_integers_are_taken_modulo_2_to_the_32(native, value):
     the missing tensors)."""
     with pytest.raises(TypeError, match="node_offsets: expected a tensor"):
         native.prepare_spec_tree(0, 0, pkg.OwlDims(), value, 1, *(None,) * 8)
+
+
+def _strided(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("call,args,message", [
+    ("kv_append", (0, 0), "expected 14 arguments"),
+    ("kv_append_fp8", (0, 0), "expected 15 arguments"),
+    ("kv_commit_fp8", (0, 0), "expected 11 arguments"),
+    ("token_logprobs", (0, 0), "expected 13 arguments"),
+    ("kv_append", (0, 0, pkg.OwlDims()) + (None,) * 11, "k: expected a tensor"),
+    ("kv_append", (0, 0, pkg.OwlDims(), None, torch.zeros(1)) + (None,) * 9, "k: expected torch.bfloat16 or torch.float16, got Float"),
+    ("kv_append", (0, 0, pkg.OwlDims(1, 4, 4, 4, 2), None, _strided(4, 2, 128)) + (None,) * 9, r"k: expected torch.bfloat16 tensor \[4, 2, 128\] on cuda:0"),
+    ("kv_commit_fp8", (0, 0, pkg.OwlDims(), torch.zeros(4, dtype=torch.uint8)) + (None,) * 7, "k_cache: expected contiguous torch.float8_e4m3fn"),
+    ("token_logprobs", (0, 0, pkg.OwlDims(), 3, torch.zeros(4, dtype=torch.int32)) + (None,) * 8, "logits: expected torch.bfloat16, torch.float32"),
+    ("token_logprobs", (0, 0, pkg.OwlDims(), 3, torch.zeros(4)) + (None,) * 8, "logits: expected contiguous torch.float32 tensor on cuda:0"),
+])
+def test_bad_arguments_of_the_cache_and_score_calls(native, call, args, message):
+    with pytest.raises(TypeError, match=message):
+        getattr(native, call)(*args)
