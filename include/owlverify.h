@@ -284,6 +284,16 @@ int owl_kv_append_fp8(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const v
                       const int32_t* block_table, const int32_t* ctx_lens, const int32_t* node_offsets, void* stream);
 
 /*
+ * owl_verify_attn over the 8-bit cache: q and out are of `dtype` (OWL_DTYPE_BF16 or OWL_DTYPE_F16), everything else as there, with
+ * the caches' values for K and V.  A block's values enter both products as fp16 numbers, exact but for what lies below 2^-24; a
+ * row of q enters divided by a power of two; the softmax weights are rounded to fp16, and the normaliser sums the rounded ones.
+ * page_exp 2-byte aligned.
+ */
+int owl_verify_attn_fp8(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void* q, const void* k_cache,
+                        const void* v_cache, const int8_t* page_exp, const int32_t* block_table, const int32_t* ctx_lens,
+                        const int32_t* node_offsets, const int32_t* tree_parent, void* out, float* lse, void* stream);
+
+/*
  * owl_kv_commit in the 8-bit cache.  A page that rows move to takes the larger of its exponent and what those rows need; if it
  * grows, the rows that stay on it (the context's and accepted ones in place already) are re-encoded.  Other slots keep their
  * bytes.

@@ -181,6 +181,13 @@ class OwlContext:
                                    node_offsets)
         return self._done(rc, check, "owl_kv_append_fp8")
 
+    def owl_verify_attn_fp8(self, dims: OwlDims, q, k_cache, v_cache, page_exp, block_table, ctx_lens, node_offsets, tree_parent, out, lse,
+                            check: bool = True) -> int:
+        """Attention over float8_e4m3fn caches; ``q`` and ``out`` both bfloat16 or both float16."""
+        rc = _native.verify_attn_fp8(self._handle, self._dev, dims, q, k_cache, v_cache, page_exp, block_table, ctx_lens, node_offsets, tree_parent,
+                                     out, lse)
+        return self._done(rc, check, "owl_verify_attn_fp8")
+
     def owl_kv_commit_fp8(self, dims: OwlDims, k_cache, v_cache, page_exp, block_table, ctx_lens, node_offsets, accept_len, accept_path,
                           check: bool = True) -> int:
         rc = _native.kv_commit_fp8(self._handle, self._dev, dims, k_cache, v_cache, page_exp, block_table, ctx_lens, node_offsets, accept_len, accept_path)

@@ -45,4 +45,17 @@ inline int make_kv_tensor_map(EncodeTiledFn encode, CUtensorMap* map, const void
     return (int)r;
 }
 
+// The 8-bit cache, [num_pages, Hkv, page_size, 128] bytes: a box is one (page, head) block as it lies, page_size rows of 128 bytes, the
+// 16-byte pieces of row r at places (piece ^ (r & 7)) by the 128-byte swizzle.
+inline int make_kv8_tensor_map(EncodeTiledFn encode, CUtensorMap* map, const void* cache, long long num_pages, int num_kv_heads, int page_size) {
+    if (!encode) return -1;
+    const cuuint64_t dims[3] = {128, (cuuint64_t)page_size, (cuuint64_t)(num_pages * num_kv_heads)};
+    const cuuint64_t strides[2] = {128, (cuuint64_t)page_size * 128};
+    const cuuint32_t box[3] = {128, (cuuint32_t)page_size, 1};
+    const cuuint32_t elem_strides[3] = {1, 1, 1};
+    return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(cache), dims, strides, box, elem_strides,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 }  // namespace owl

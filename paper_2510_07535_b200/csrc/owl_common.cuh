@@ -50,6 +50,7 @@ struct AttnParams {
     int32_t combine_group;        // partials per round of the merge kernel, 4..32
     int32_t combine_lg_parts;     // log2 of the CTAs that share a block's channels
     int32_t combine_row_ctas;     // the merge kernel's CTAs that take rows (persistent)
+    const int8_t* page_exp;       // 8-bit cache: [num_pages, Hkv, 2] exponents of K and V
     int32_t f16;                  // q / caches / out are fp16 instead of bf16 (same size; typed as bf16 pointers here)
     float sm_scale;
 };

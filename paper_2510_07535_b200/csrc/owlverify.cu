@@ -18,11 +18,13 @@
 #include "logprobs.cuh"
 #include "owl_common.cuh"
 #include "spec_loop.cuh"
+#include "verify_attn_fp8.cuh"
 #include "verify_attn_umma.cuh"
 
 using namespace owl;
 
 constexpr int kMapCacheEntries = 8;
+enum CacheType { kCacheBf16, kCacheF16, kCacheFp8 };
 
 struct owl_ctx {
     int device = 0;
@@ -51,7 +53,7 @@ struct owl_ctx {
         const void* k = nullptr;
         const void* v = nullptr;
         int pages = 0, heads = 0, page_size = 0;
-        bool fp16 = false;
+        CacheType type = kCacheBf16;
         uint64_t used = 0;
     } maps[kMapCacheEntries];
     uint64_t map_clock = 0;
@@ -117,6 +119,17 @@ UmmaKernel umma_kernel(bool many, bool wide, bool fused, bool fp16) {
         {verify_attn_umma_kernel<true, false, false, true>, verify_attn_umma_kernel<true, true, false, true>}};
     return fp16 ? table16[many][wide] : table[many][wide][fused];
 }
+// Those over the 8-bit cache: [block-wide schedule][units above 128 rows][fp16 queries]
+using Fp8Kernel = void (*)(AttnParams, CUtensorMap, CUtensorMap);
+Fp8Kernel fp8_kernel(bool many, bool wide, bool fp16) {
+    using namespace umma_path;
+    static const Fp8Kernel table[2][2][2] = {
+        {{verify_attn_fp8_kernel<false, false, false>, verify_attn_fp8_kernel<false, false, true>},
+         {verify_attn_fp8_kernel<false, true, false>, verify_attn_fp8_kernel<false, true, true>}},
+        {{verify_attn_fp8_kernel<true, false, false>, verify_attn_fp8_kernel<true, false, true>},
+         {verify_attn_fp8_kernel<true, true, false>, verify_attn_fp8_kernel<true, true, true>}}};
+    return table[many][wide][fp16];
+}
 // The merge kernel's: [acceptance walk in extra CTAs][the pass's schedule read from global memory]
 using CombineKernel = void (*)(AttnParams, AcceptParams);
 CombineKernel combine_kernel(bool fused, bool many) {
@@ -130,6 +143,9 @@ bool set_umma_smem_attr() {
                                         umma_path::kSmemBytes) == cudaSuccess;
     for (int i = 0; i < 4; ++i)
         ok = ok && cudaFuncSetAttribute(umma_kernel(i & 2, i & 1, false, true), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        umma_path::kSmemBytes) == cudaSuccess;
+    for (int i = 0; i < 8; ++i)
+        ok = ok && cudaFuncSetAttribute(fp8_kernel(i & 4, i & 2, i & 1), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                         umma_path::kSmemBytes) == cudaSuccess;
     return ok;
 }
@@ -381,7 +397,7 @@ static void launch_accept(owl_ctx* ctx, AcceptParams& p, cudaStream_t stream);
 static int verify_attn_impl(owl_ctx* ctx, const owl_dims* d, const void* q, const void* k_cache, const void* v_cache,
                             const int32_t* block_table, const int32_t* ctx_lens, const int32_t* node_offsets,
                             const int32_t* tree_parent, void* out, float* lse, void* stream_, AcceptParams* ap,
-                            bool fp16 = false, bool own_scan = false) {
+                            bool fp16 = false, bool own_scan = false, const int8_t* page_exp = nullptr) {
     if (!ctx) return OWL_ERR_INVALID_ARG;
     int rc = check_dims(d, true, false);
     if (rc != OWL_OK) return rc;
@@ -425,18 +441,23 @@ static int verify_attn_impl(owl_ctx* ctx, const owl_dims* d, const void* q, cons
     p.num_ctas = ctx->num_ctas;
     p.sm_scale = d->sm_scale;
     p.f16 = fp16 ? 1 : 0;
+    p.page_exp = page_exp;
+    const CacheType type = page_exp ? kCacheFp8 : fp16 ? kCacheF16 : kCacheBf16;
 
     owl_ctx::MapEntry* maps = nullptr;
     {
         owl_ctx::MapEntry* lru = &ctx->maps[0];
         for (auto& m : ctx->maps) {
             if (m.k == k_cache && m.v == v_cache && m.pages == d->num_pages && m.heads == d->num_kv_heads &&
-                m.page_size == d->page_size && m.fp16 == fp16) { maps = &m; break; }
+                m.page_size == d->page_size && m.type == type) { maps = &m; break; }
             if (m.used < lru->used) lru = &m;
         }
         if (!maps) {
-            const int rk = make_kv_tensor_map(ctx->encode, &lru->kmap, k_cache, d->num_pages, d->num_kv_heads, d->page_size, fp16);
-            const int rv = make_kv_tensor_map(ctx->encode, &lru->vmap, v_cache, d->num_pages, d->num_kv_heads, d->page_size, fp16);
+            auto encode = [&](CUtensorMap* map, const void* cache) {
+                return page_exp ? make_kv8_tensor_map(ctx->encode, map, cache, d->num_pages, d->num_kv_heads, d->page_size)
+                                : make_kv_tensor_map(ctx->encode, map, cache, d->num_pages, d->num_kv_heads, d->page_size, fp16);
+            };
+            const int rk = encode(&lru->kmap, k_cache), rv = encode(&lru->vmap, v_cache);
             if (rk != 0 || rv != 0) {
                 lru->k = lru->v = nullptr;
                 lru->used = 0;
@@ -444,7 +465,7 @@ static int verify_attn_impl(owl_ctx* ctx, const owl_dims* d, const void* q, cons
                 return OWL_ERR_CUDA;
             }
             lru->k = k_cache; lru->v = v_cache;
-            lru->pages = d->num_pages; lru->heads = d->num_kv_heads; lru->page_size = d->page_size; lru->fp16 = fp16;
+            lru->pages = d->num_pages; lru->heads = d->num_kv_heads; lru->page_size = d->page_size; lru->type = type;
             maps = lru;
         }
         maps->used = ++ctx->map_clock;
@@ -466,7 +487,7 @@ static int verify_attn_impl(owl_ctx* ctx, const owl_dims* d, const void* q, cons
     {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(ctx->num_ctas);
-        cfg.blockDim = dim3(umma_path::kThreads);
+        cfg.blockDim = dim3(page_exp ? umma_path::kFp8Threads : umma_path::kThreads);
         cfg.dynamicSmemBytes = umma_path::kSmemBytes;
         cfg.stream = stream;
         cudaLaunchAttribute attr[1];
@@ -477,7 +498,8 @@ static int verify_attn_impl(owl_ctx* ctx, const owl_dims* d, const void* q, cons
         // the instance that holds only this call's case: block-wide schedule unless the line is short (small_schedule), the two-row-block
         // mode only if a unit (G * max_nodes rows at most) can exceed 128 rows, the logits scan only in a step
         const bool many = !p.small, wide = G * d->max_nodes > 128;
-        cudaLaunchKernelEx(&cfg, umma_kernel(many, wide, ap && !own_scan, fp16), p, maps->kmap, maps->vmap, ap ? *ap : AcceptParams{});
+        if (page_exp) cudaLaunchKernelEx(&cfg, fp8_kernel(many, wide, fp16), p, maps->kmap, maps->vmap);
+        else cudaLaunchKernelEx(&cfg, umma_kernel(many, wide, ap && !own_scan, fp16), p, maps->kmap, maps->vmap, ap ? *ap : AcceptParams{});
     }
     ++ctx->launches;
     if (ctx->profiling) cudaEventRecord(ctx->ev[1], stream);
@@ -509,6 +531,14 @@ int owl_verify_attn_f16(owl_ctx* ctx, const owl_dims* d, const void* q, const vo
                         const int32_t* tree_parent, void* out, float* lse, void* stream_) {
     return verify_attn_impl(ctx, d, q, k_cache, v_cache, block_table, ctx_lens, node_offsets, tree_parent, out, lse, stream_,
                             nullptr, true);
+}
+
+int owl_verify_attn_fp8(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const void* q, const void* k_cache, const void* v_cache,
+                        const int8_t* page_exp, const int32_t* block_table, const int32_t* ctx_lens, const int32_t* node_offsets,
+                        const int32_t* tree_parent, void* out, float* lse, void* stream_) {
+    if (!page_exp || (reinterpret_cast<uintptr_t>(page_exp) & 1u) || (dtype != OWL_DTYPE_BF16 && dtype != OWL_DTYPE_F16)) return OWL_ERR_INVALID_ARG;
+    return verify_attn_impl(ctx, d, q, k_cache, v_cache, block_table, ctx_lens, node_offsets, tree_parent, out, lse, stream_,
+                            nullptr, dtype == OWL_DTYPE_F16, false, page_exp);
 }
 
 // Argument checks of the acceptance and its kernel parameters.

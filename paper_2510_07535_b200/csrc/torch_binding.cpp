@@ -291,6 +291,24 @@ PyObject* append_call(PyObject* const* args, Py_ssize_t nargs, bool fp8) {
 }
 OWL_CALL(kv_append) { return append_call(args, nargs, false); }
 OWL_CALL(kv_append_fp8) { return append_call(args, nargs, true); }
+// (handle, device, dims, tensors); the element type is q's
+OWL_CALL(verify_attn_fp8) {
+    Head h;
+    owl_dims d;
+    int dtype;
+    Type type;
+    void* p[10];
+    if (!h.parse(args, nargs, 13) || !dims_of(args[2], &d) || !dtype_of(args[3], "q", false, &type, &dtype)) return nullptr;
+    const Spec s[] = {{"q", type}, {"k_cache", kE4m3}, {"v_cache", kE4m3}, {"page_exp", kI8}, {"block_table", kI32}, {"ctx_lens", kI32},
+                      {"node_offsets", kI32}, {"tree_parent", kI32}, {"out", type}, {"lse", kF32}};
+    if (!tensors(args + 3, s, 10, h.device, p)) return nullptr;
+    auto i = [&](int n) { return static_cast<int32_t*>(p[n]); };
+    void* stream = h.stream();
+    return unlocked([&] {
+        return owl_verify_attn_fp8(h.ctx, &d, dtype, p[0], p[1], p[2], static_cast<int8_t*>(p[3]), i(4), i(5), i(6), i(7), p[8],
+                                   static_cast<float*>(p[9]), stream);
+    });
+}
 OWL_CALL(kv_commit_fp8) {
     static const Spec s[] = {{"k_cache", kE4m3}, {"v_cache", kE4m3}, {"page_exp", kI8}, {"block_table", kI32}, {"ctx_lens", kI32},
                              {"node_offsets", kI32}, {"accept_len", kI32}, {"accept_path", kI32}};
@@ -338,7 +356,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 PyMethodDef methods[] = {OWL_METHOD(verify_attn), OWL_METHOD(verify_attn_f16), OWL_METHOD(tree_accept), OWL_METHOD(tree_accept_spec),
                          OWL_METHOD(verify_step), OWL_METHOD(kv_commit), OWL_METHOD(prepare_spec_tree), OWL_METHOD(prepare_hybrid),
                          OWL_METHOD(lm_head_accept), OWL_METHOD(lstm_cell), OWL_METHOD(tree_accept_static), OWL_METHOD(kv_append),
-                         OWL_METHOD(kv_append_fp8), OWL_METHOD(kv_commit_fp8), OWL_METHOD(token_logprobs), {nullptr, nullptr, 0, nullptr}};
+                         OWL_METHOD(kv_append_fp8), OWL_METHOD(verify_attn_fp8), OWL_METHOD(kv_commit_fp8), OWL_METHOD(token_logprobs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_owl_native", "Tensor marshalling for libowlverify", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

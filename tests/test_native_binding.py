@@ -66,6 +66,8 @@ def _strided(*shape):
     ("kv_append", (0, 0), "expected 14 arguments"),
     ("kv_append_fp8", (0, 0), "expected 15 arguments"),
     ("kv_commit_fp8", (0, 0), "expected 11 arguments"),
+    ("verify_attn_fp8", (0, 0), "expected 13 arguments"),
+    ("verify_attn_fp8", (0, 0, pkg.OwlDims(), torch.zeros(4)) + (None,) * 9, "q: expected torch.bfloat16 or torch.float16, got Float"),
     ("token_logprobs", (0, 0), "expected 13 arguments"),
     ("kv_append", (0, 0, pkg.OwlDims()) + (None,) * 11, "k: expected a tensor"),
     ("kv_append", (0, 0, pkg.OwlDims(), None, torch.zeros(1)) + (None,) * 9, "k: expected torch.bfloat16 or torch.float16, got Float"),
