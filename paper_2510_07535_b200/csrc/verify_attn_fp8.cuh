@@ -1,17 +1,32 @@
-// Verify attention over the 8-bit cache (fp8_block.cuh): the pass of verify_attn_umma.cuh - its partition, segments, products, softmax
-// and partials - with four more warps between the copies and the products.
+// Verify attention over the 8-bit cache (fp8_block.cuh).  Partition, segments, partials and the order of events are those of
+// verify_attn_umma.cuh; what differs follows from K and V arriving as e4m3.
 //
-//   warp 0        TMA producer: one box per (page, head) of K and of V into a ring of 16 KB raw slots; leaves each tile's exponents
-//   warp 1        issues the products (mma_loop)
-//   warps 4-11    softmax (softmax_loop)
-//   warps 12-15   turn a raw slot into an fp16 operand tile: e4m3 * 2^e is an fp16 number, so nothing is rounded (but what lies
-//                 below fp16's smallest step, 2^-24), and both products are the 16-bit ones of the 16-bit caches, exact in their operands.
-//                 (Products of 8-bit operands straight from the raw slots would need queries and weights cut into e4m3
-//                 pieces: twice the instructions at twice the rate, and weights below 2^-15 of the largest would be lost, which
-//                 is where a long context's mass may lie beside one dominant key.)
+//   S = Q K^T   on 8-bit operands, K straight from where TMA put it.  A row of Q, divided by a power of two, is cut into e4m3 pieces, each
+//               the remainder of those before: two for bf16 queries (eight significant bits, four a piece), three for fp16 ones.
+//               The pieces' products add up in one accumulator.  What the pieces leave of an element is below half of e4m3's smallest step,
+//               2^-10, where the row's largest element is above 224: 2^-17.8 of that largest element.  A block's 2^e multiplies its
+//               columns of S, along with sm_scale, in fp32.
+//   O += P V    on fp16 operands: four warps turn a V tile into fp16, 2^e included (exact but for what lies below fp16's smallest
+//               step, 2^-24), and the weights are fp16.  Weights cut into e4m3 pieces would lose what is below 2^-15 of the largest, which
+//               is where a long context's mass may lie beside one dominant key.
 //
-// HBM brings half the bytes of a 16-bit cache; what a tile costs the SM in shared-memory traffic is more than there: 32 KB written by TMA,
-// 32 read and 64 written by the conversion, then Q, K and V as operands.
+// Two e4m3 products of 128x128x32 take the time of one fp16 pair, so the tensor pipe does the work of the 16-bit caches' pass; HBM brings half
+// of its bytes, and shared memory carries per tile 32 KB from TMA, 64 for Q K^T, 16 + 32 for the conversion and 32 for P V.  (A
+// form that turned K into fp16 as well moved 224 KB, kept the ring half as deep, and took 453 instead of %CH% us on 16 chains of 8 at 4K to 64K.)
+//
+// 16 warps:
+//   warp 0        TMA producer: one box per (page, head) of K and of V into a ring of tiles of 2 x 16 KB; leaves each tile's note
+//   warp 1        issues the products
+//   warps 4-11    softmax, two streams
+//   warps 12-15   turn V into fp16, two slots of 32 KB
+//
+// Which operand has the lanes.  Units of more than 64 rows: the rows of Q (S and P as in verify_attn_umma.cuh, P in tensor memory).  Units of
+// up to 64 rows ("keys on lanes"): the products are turned round,
+//   S^T = K Q^T   [128 keys x pieces * rows], the pieces' columns added up in registers,
+//   O^T += V^T P  [128 channels x rows],      P [keys x rows] through shared memory,
+// so that a unit of 32 rows does not pay for 128 of them: the products take an eighth and a quarter of the multipliers (and of the power,
+// which is what sets the clock here), a softmax thread has one key and all rows, every lane is in use, and sums over keys are
+// kept per thread until the segment's end.
 #pragma once
 
 #include "fp8_block.cuh"
@@ -21,22 +36,68 @@ namespace owl {
 namespace umma_path {
 
 constexpr int kFp8Threads = 512;
-constexpr int kRawBytes = kTileKeys * kHeadDim;      // 16 KB
-template <bool kWide> constexpr int kRawSlots = kWide ? 2 : kFp8RawSlots;
-template <bool kWide> constexpr int kRawOff = kRingOff<kWide> + kFp8Slots * kSlotBytes;
-static_assert(kRawOff<false> + kRawSlots<false> * kRawBytes == kAuxOff && kRawOff<true> + kRawSlots<true> * kRawBytes == kAuxOff, "layout");
+constexpr int kPieceBytes = 128 * kHeadDim;          // 16 KB: one piece of 128 rows of Q; also a raw K or V tile
+constexpr int kFp8VSlots = 2;                        // fp16 V tiles, 32 KB each
+constexpr int kNotes = 8;
+constexpr int kRowsOfPartial = kRows;                // (`kRows` below is also a parameter's name)
+constexpr int kKeysRows = 64;                        // most rows of a unit with its keys on the lanes
+constexpr int kPBytes = kTileKeys * 128;             // its P: 128 bytes (64 rows) per key, one per stream
+// Shared memory: Q (its pieces; keys on lanes: fewer rows, then the two P), the fp16 V tiles, the ring of raw tiles, scratch.
+template <bool kF16> constexpr int kPieces = kF16 ? 3 : 2;
+template <bool kF16> constexpr int kPOff = kPieces<kF16> * kKeysRows * kHeadDim;
+constexpr int larger(int a, int b) { return a > b ? a : b; }
+template <bool kWide, bool kF16> constexpr int kVOff = larger((kWide ? 2 : 1) * kPieces<kF16> * kPieceBytes, kPOff<kF16> + 2 * kPBytes);
+template <bool kWide, bool kF16> constexpr int kRawOff = kVOff<kWide, kF16> + kFp8VSlots * kSlotBytes;
+template <bool kWide, bool kF16> constexpr int kRawTiles = (kAuxOff - kRawOff<kWide, kF16>) / (2 * kPieceBytes);
+static_assert(kRawTiles<false, false> == 3 && kRawTiles<false, true> == 3 && kRawTiles<true, false> == 3 && kRawTiles<true, true> == 2, "layout");
+// Keys on lanes: the rows' numbers, one set per stream.
+struct KeysScratch {
+    float scale[2][kKeysRows], bias[2][kKeysRows];   // a weight is exp2(score * scale + bias)
+    float m[2][kKeysRows], alpha[2][32];
+    unsigned most[2][32];                            // largest score of the tile, as an ordered integer
+    float sum[2][4][kKeysRows];                      // of the weights, by warp
+    float w[2][kKeysRows];                           // what the streams' O are multiplied by
+};
+template <bool kWide, bool kF16> constexpr int kScratchOff = kWide ? kPOff<kF16> + 2 * kPBytes : kRawOff<kWide, kF16> + kRawTiles<kWide, kF16> * 2 * kPieceBytes;
+static_assert(kScratchOff<false, false> + sizeof(KeysScratch) <= kAuxOff && kScratchOff<false, true> + sizeof(KeysScratch) <= kAuxOff, "layout");
+static_assert(kScratchOff<true, false> + sizeof(KeysScratch) <= kVOff<true, false> && kScratchOff<true, true> + sizeof(KeysScratch) <= kVOff<true, true>, "layout");
+// Tensor memory: S0 S1 O0 O1 of 128 columns; keys on lanes: two S of up to 192, two O of 64.
+constexpr uint32_t kKeysS = 192, kKeysO = 384;
 
-template <bool kWide, bool kManySeqs>
+// What is known of a tile besides its bytes.  A place is written again eight tiles later: the producer is at most kRawTiles ahead of
+// the products, and those one tile per stream ahead of the softmax warps, the last to look at it.
+struct TileNote {
+    float kscale[kTileKeys / 16];                // 2^e of K, for each 16 keys
+    int valid;                                   // keys of the sequence in it; -1: no more tiles
+    int8_t vexp[kTileKeys / 16];                 // e of V
+};
+struct AuxFp8 : Aux {
+    uint64_t raw_full[8], raw_empty[8];          // K and V of each raw tile
+    uint64_t v_full[kFp8VSlots], v_empty[kFp8VSlots];
+    TileNote note[kNotes];
+    float row_scale[kRows];                      // what the rows of Q were divided by
+};
+static_assert(sizeof(AuxFp8) <= kAuxBytes, "aux area too small");
+static_assert(kNotes >= 4 + 2, "a note outlives its tile's place in the ring");
+
+// Rows that a unit with its keys on the lanes is padded to; 0: its rows are on the lanes.
+__device__ __forceinline__ int keys_rows(int M) { return M <= 32 ? 32 : M <= kKeysRows ? 64 : 0; }
+// Warps of a stream's warpgroup with something to do in a unit of up to 128 rows.
+__device__ __forceinline__ int live_warps_fp8(int M) { return M <= kKeysRows ? 4 : (M + 31) >> 5; }
+
+// ------------------------------------------------------------------------------------------ producer
+template <bool kWide, bool kF16, bool kManySeqs>
 __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUtensorMap* kmap, const CUtensorMap* vmap, AuxFp8* aux,
                                                   uint32_t raw, Walker<kManySeqs> w) {
-    constexpr uint32_t kPlaces = kRawSlots<kWide> / 2;
+    constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
     const int lane = threadIdx.x & 31;
     volatile int* abort_flag = &aux->abort_flag;
     const int ppt = kTileKeys >> p.page_shift;               // pages (= TMA boxes) per tile
+    const int block_tiles = 32 / ppt;
     const uint32_t box_bytes = (uint32_t)p.page_size * 128u;
     const int oob = p.num_pages * p.num_kv_heads;            // a coordinate past the end: the box reads zeros
     const uint64_t stream_policy = l2_policy_evict_first();
-    uint32_t place = 0, free_parity = 1;
+    uint32_t place = 0, free_parity = 1, seq = 0;
     for (uint32_t seg_no = 0;; ++seg_no) {
         Segment g;
         g.b = g.n = g.L = 0;
@@ -44,16 +105,17 @@ __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUt
         const int keys = g.L + g.n;
         const int pages_valid = (keys + p.page_size - 1) >> p.page_shift;
         const int32_t* table = p.block_table + (long long)g.b * p.max_pages_per_seq;
-        auto page_of = [&](int t) {
+        // 32 pages of the table at a time, one per lane: those of the tiles from `t` on.  Pages are asked for two such blocks ahead and their
+        // exponents (K's in the low byte, V's in the high one) one block ahead, which is four tiles with the smallest pages: an
+        // exponent is a load that waits for a load.
+        auto pages_of = [&](int t) {
             const int lp = t * ppt + lane;
-            return lane < ppt && lp < pages_valid ? table[lp] : -1;
+            return t < g.tile1 && lp < pages_valid ? table[lp] : -1;
         };
-        // K's exponent in the low byte, V's in the high one
         auto exps_of = [&](int pg) -> int {
             return (unsigned)pg < (unsigned)p.num_pages ? *reinterpret_cast<const uint16_t*>(p.page_exp + ((long long)pg * p.num_kv_heads + g.h) * 2) : 0;
         };
-        // pages are asked for two tiles ahead and their exponents one tile ahead
-        int page_cur = more ? page_of(g.tile0) : -1, page_next = more && g.tile0 + 1 < g.tile1 ? page_of(g.tile0 + 1) : -1;
+        int pages = more ? pages_of(g.tile0) : -1, pages_next = more ? pages_of(g.tile0 + block_tiles) : -1;
         if (seg_no >= (uint32_t)kSegs && !readers_reached(aux, (int)seg_no - kSegs + 1)) break;
         Segment& announced = aux->seg[seg_no % kSegs];
         if (lane == 0) {
@@ -64,112 +126,964 @@ __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUt
         }
         __syncwarp();
         if (!more) break;
-        int exps_cur = exps_of(page_cur);
-        for (int t = g.tile0; t < g.tile1; ++t) {
+        int exps = exps_of(pages), exps_next = 0, pages_after = -1;
+        for (int t = g.tile0, in_block = 0; t < g.tile1; ++t) {
+            if (in_block == 0) {
+                exps_next = exps_of(pages_next);
+                pages_after = pages_of(t + 2 * block_tiles);
+            }
+            const int page = __shfl_sync(0xffffffffu, pages, in_block * ppt + lane);      // of the tile's pages, this lane's (lanes below ppt)
             int coord = oob;
-            if ((unsigned)page_cur < (unsigned)p.num_pages) coord = page_cur * p.num_kv_heads + g.h;
+            if ((unsigned)page < (unsigned)p.num_pages) coord = page * p.num_kv_heads + g.h;
             else if (lane < ppt && t * ppt + lane < pages_valid) {
                 report(p.status, kErrBadPage);
                 const_cast<volatile int&>(announced.bad_page) = 1;
             }
-            const int exps_next = exps_of(page_next);
-            const int page_after = t + 2 < g.tile1 ? page_of(t + 2) : -1;
             bool ok = true;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 const uint32_t slot = 2u * place + kv, full = smem_u32(&aux->raw_full[slot]);
-                ok = mbar_wait(smem_u32(&aux->raw_empty[slot]), free_parity, abort_flag) && ok;
-                if (ok && lane == 0) mbar_arrive_expect_tx(full, (uint32_t)kRawBytes);
+                // (one verdict for the warp: its lanes go on together)
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&aux->raw_empty[slot]), free_parity, abort_flag)) && ok;
+                if (ok && lane == 0) mbar_arrive_expect_tx(full, (uint32_t)kPieceBytes);
                 __syncwarp();
                 if (ok && lane < ppt)
-                    tma_load_3d_hint(raw + slot * kRawBytes + lane * box_bytes, kv ? vmap : kmap, full, 0, 0, coord, stream_policy);
+                    tma_load_3d_hint(raw + slot * kPieceBytes + lane * box_bytes, kv ? vmap : kmap, full, 0, 0, coord, stream_policy);
                 __syncwarp();
             }
-            // V's slot is free, so the warps that read this place's note are done with it; the K slot's barrier expects one more arrival
-            TileNote& note = aux->note[place];
-            if (lane < ppt) {
-                note.exp[0][lane] = (int8_t)(exps_cur & 0xff);
-                note.exp[1][lane] = (int8_t)(exps_cur >> 8);
+            // the note: an arrival of its own on both barriers, after the copies have been asked for
+            TileNote& note = aux->note[seq % kNotes];
+            const int exp_kv = __shfl_sync(0xffffffffu, exps, in_block * ppt + ((lane * 16) >> p.page_shift));
+            if (lane < kTileKeys / 16) {
+                note.kscale[lane] = exp2_int(max(kExpMin, min(kExpMax, (int)(int8_t)(exp_kv & 0xff))));
+                note.vexp[lane] = (int8_t)(exp_kv >> 8);
             }
             if (lane == 0) note.valid = min(kTileKeys, keys - t * kTileKeys);
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&aux->raw_full[2u * place]));
-            page_cur = page_next; page_next = page_after; exps_cur = exps_next;
+            if (lane < 2) mbar_arrive(smem_u32(&aux->raw_full[2u * place + lane]));
+            if (++in_block == block_tiles) { in_block = 0; pages = pages_next; exps = exps_next; pages_next = pages_after; }
             if (++place == kPlaces) { place = 0; free_parity ^= 1u; }
+            ++seq;
         }
     }
     // no more tiles (after a wait that gave up the converting warps stop by themselves)
-    const bool ok = mbar_wait(smem_u32(&aux->raw_empty[2u * place]), free_parity, abort_flag) &&
-                    mbar_wait(smem_u32(&aux->raw_empty[2u * place + 1u]), free_parity, abort_flag);
+    const bool ok = mbar_wait(smem_u32(&aux->raw_empty[2u * place + 1u]), free_parity, abort_flag);
     if (lane == 0 && ok) {
-        aux->note[place].valid = -1;
-        mbar_arrive(smem_u32(&aux->raw_full[2u * place]));
-        mbar_arrive(smem_u32(&aux->raw_full[2u * place]));
+        aux->note[seq % kNotes].valid = -1;
+        mbar_arrive(smem_u32(&aux->raw_full[2u * place + 1u]));
+        mbar_arrive(smem_u32(&aux->raw_full[2u * place + 1u]));
     }
 }
 
-// ------------------------------------------------------------------------------------------ conversion
+// ------------------------------------------------------------------------------------------ V to fp16
 // Warp w of four takes key groups 4w .. 4w + 3 of a tile, eight keys x 64 elements per turn.  Lane: 16 elements (one 16-byte piece) of
 // one key.  Raw rows are 128 bytes with piece x at place x ^ (key & 7), operand rows 128 bytes per half of the head dimension with
 // piece y at y ^ (key & 7), and a raw piece becomes operand pieces 2x, 2x + 1: eight neighbouring lanes take four pieces of two keys
 // that differ in bits 0 and 2, so that neither the loads nor the stores meet in a bank.
-template <bool kWide>
+template <bool kWide, bool kF16>
 __device__ __forceinline__ void convert_loop(const AttnParams& p, AuxFp8* aux, unsigned char* smem) {
-    constexpr uint32_t kPlaces = kRawSlots<kWide> / 2;
+    constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
     constexpr unsigned kAll = 0xffffffffu;
     volatile int* abort_flag = &aux->abort_flag;
     const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
     const int r = lane >> 2, key7 = (r >> 1) ^ ((r & 1) * 5), piece = lane & 3;
-    const unsigned char* raw = smem + kRawOff<kWide> + warp * 4096 + key7 * 128;
-    unsigned char* ring = smem + kRingOff<kWide> + warp * 8192 + key7 * 128;
+    const unsigned char* raw = smem + kRawOff<kWide, kF16> + kPieceBytes + warp * 4096 + key7 * 128;
+    unsigned char* ring = smem + kVOff<kWide, kF16> + warp * 8192 + key7 * 128;
+    uint32_t place = 0, parity = 0;
     for (uint32_t n = 0;; ++n) {
-        const uint32_t place = n % kPlaces, parity = (n / kPlaces) & 1u;
-        if (!__all_sync(kAll, mbar_wait(smem_u32(&aux->raw_full[2u * place]), parity, abort_flag))) return;
-        const TileNote& note = aux->note[place];
+        if (!__all_sync(kAll, mbar_wait(smem_u32(&aux->raw_full[2u * place + 1u]), parity, abort_flag))) return;
+        const TileNote& note = aux->note[n % kNotes];
         const int valid = const_cast<const volatile int&>(note.valid);
         if (valid < 0) return;
-#pragma unroll 1
-        for (uint32_t kv = 0; kv < 2; ++kv) {
-            const uint32_t slot = 2u * (n % kFp8Places) + kv;
-            bool ok = kv == 0 || mbar_wait(smem_u32(&aux->raw_full[2u * place + 1u]), parity, abort_flag);
-            ok = mbar_wait(smem_u32(&aux->empty[slot]), ((n / kFp8Places) & 1u) ^ 1u, abort_flag) && ok;
-            if (!__all_sync(kAll, ok)) return;
-            const unsigned char* src = raw + (2u * place + kv) * kRawBytes;
-            unsigned char* dst = ring + slot * kSlotBytes;
-            uint4 u[8];
+        const uint32_t slot = n % kFp8VSlots;
+        if (!__all_sync(kAll, mbar_wait(smem_u32(&aux->v_empty[slot]), ((n / kFp8VSlots) & 1u) ^ 1u, abort_flag))) return;
+        const unsigned char* src = raw + 2u * place * kPieceBytes;
+        unsigned char* dst = ring + slot * kSlotBytes;
+        uint4 u[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                u[j] = *reinterpret_cast<const uint4*>(src + (j >> 1) * 1024 + ((((j & 1) * 4 + piece) ^ key7) << 4));
+        for (int j = 0; j < 8; ++j)
+            u[j] = *reinterpret_cast<const uint4*>(src + (j >> 1) * 1024 + ((((j & 1) * 4 + piece) ^ key7) << 4));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int key = (4 * warp + (j >> 1)) * 8;             // of the group's first key
-                const int e = max(kExpMin, min(kExpMax, (int)note.exp[kv][key >> p.page_shift]));
-                const uint32_t one = e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24);
-                const uint32_t two_to_e = one | one << 16;
-                uint32_t o[8];
-                const uint32_t w[4] = {u[j].x, u[j].y, u[j].z, u[j].w};
+        for (int j = 0; j < 8; ++j) {
+            const int group = 4 * warp + (j >> 1);                     // of eight keys
+            const int e = max(kExpMin, min(kExpMax, (int)note.vexp[group >> 1]));
+            const uint32_t one = e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24);
+            const uint32_t two_to_e = one | one << 16;
+            uint32_t o[8];
+            const uint32_t w[4] = {u[j].x, u[j].y, u[j].z, u[j].w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t a = e4m3x2_to_f16x2(w[i] & 0xffffu), b = e4m3x2_to_f16x2(w[i] >> 16);
-                    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i]) : "r"(a), "r"(two_to_e));
-                    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i + 1]) : "r"(b), "r"(two_to_e));
-                }
-                // V rows past the sequence's end may hold anything, and their weight of 0 does not make a NaN harmless
-                if (kv == 1 && key + key7 >= valid) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = 0u;
-                }
-                unsigned char* to = dst + (j >> 1) * 2048 + (j & 1) * 1024;
-                *reinterpret_cast<uint4*>(to + (((2 * piece) ^ key7) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-                *reinterpret_cast<uint4*>(to + (((2 * piece + 1) ^ key7) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t a = e4m3x2_to_f16x2(w[i] & 0xffffu), b = e4m3x2_to_f16x2(w[i] >> 16);
+                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i]) : "r"(a), "r"(two_to_e));
+                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i + 1]) : "r"(b), "r"(two_to_e));
             }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_u32(&aux->full16[slot]));
-                mbar_arrive(smem_u32(&aux->raw_empty[2u * place + kv]));
+            // rows past the sequence's end may hold anything, and their weight of 0 does not make a NaN harmless
+            if (group * 8 + key7 >= valid) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = 0u;
+            }
+            unsigned char* to = dst + (j >> 1) * 2048 + (j & 1) * 1024;
+            *reinterpret_cast<uint4*>(to + (((2 * piece) ^ key7) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(to + (((2 * piece + 1) ^ key7) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(smem_u32(&aux->v_full[slot]));
+            mbar_arrive(smem_u32(&aux->raw_empty[2u * place + 1u]));
+        }
+        if (++place == kPlaces) { place = 0; parity ^= 1u; }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ MMA issuer
+// mma_loop's turns and hand-offs.  K arrives in the raw ring, V apart from it as an fp16 tile; both streams on one tile (256 rows): the
+// softmax warp that looks at the next K tile for this warp also makes sure of V before it announces P.
+template <bool kWide, bool kF16>
+__device__ __forceinline__ void mma_loop_fp8(AuxFp8* aux, uint32_t smem_base, uint32_t tmem) {
+    constexpr unsigned kAll = 0xffffffffu;
+    constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
+    volatile int* abort_flag = &aux->abort_flag;
+    constexpr uint32_t idesc_qk = umma_idesc_e4m3(128, kTileKeys);
+    constexpr uint32_t idesc_pv = umma_idesc_16bit(128, kHeadDim, 0, 1, true);
+    const uint32_t elected = elect_one() ? 1u : 0u;
+    // of Q's first piece, of the first raw K tile and of the first V tile; the others differ in the start address
+    const uint64_t q_desc0 = umma_smem_desc_sw128(smem_base, 16, 1024);
+    const uint64_t k_desc0 = umma_smem_desc_sw128(smem_base + kRawOff<kWide, kF16>, 16, 1024);
+    const uint64_t v_desc0 = umma_smem_desc_sw128(smem_base + kVOff<kWide, kF16>, 1024, 2048);
+    const uint32_t q_hi = (uint32_t)(q_desc0 >> 32), k_hi = (uint32_t)(k_desc0 >> 32), v_hi = (uint32_t)(v_desc0 >> 32);
+    const uint32_t raw_full = smem_u32(&aux->raw_full[0]), raw_empty = smem_u32(&aux->raw_empty[0]);
+    const uint32_t v_full = smem_u32(&aux->v_full[0]), v_empty = smem_u32(&aux->v_empty[0]);
+    const uint32_t s_full = smem_u32(&aux->s_full[0]), o_done = smem_u32(&aux->o_done[0]);
+    uint32_t seg_no = 0, k_place = 0, k_parity = 0, v_seq = 0;
+
+    auto qk = [&](uint32_t issue, uint32_t tS, uint32_t q_lo) {
+        const uint32_t k_lo = (uint32_t)k_desc0 + k_place * (uint32_t)(2 * kPieceBytes >> 4);
+#pragma unroll
+        for (int piece = 0; piece < kPieces<kF16>; ++piece)
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+                umma_f8_ss_lh_if(issue, tS, q_lo + (uint32_t)((piece * kPieceBytes + ks * 32) >> 4), q_hi, k_lo + (uint32_t)(ks * 32 >> 4), k_hi,
+                                 idesc_qk, (piece | ks) ? 1u : 0u);
+    };
+    auto pv = [&](uint32_t issue, uint32_t tS, uint32_t accumulate) {
+        const uint32_t v_lo = (uint32_t)v_desc0 + (v_seq % kFp8VSlots) * (uint32_t)(kSlotBytes >> 4);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+            umma_ts_lh_if(issue, tS + 256, tS + ks * 8, v_lo + (uint32_t)(ks * 4096 >> 4), v_hi, idesc_pv, ks ? 1u : accumulate);
+    };
+    // keys on lanes, `rows` padded rows
+    const uint64_t p_desc0 = umma_smem_desc_sw128(smem_base + kPOff<kF16>, 1024, 1024);
+    auto qk_keys = [&](uint32_t issue, uint32_t s, uint32_t rows) {
+        const uint32_t k_lo = (uint32_t)k_desc0 + k_place * (uint32_t)(2 * kPieceBytes >> 4);
+        const uint32_t idesc = umma_idesc_e4m3(128, 0) | (kPieces<kF16> * rows >> 3) << 17;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+            umma_f8_ss_lh_if(issue, tmem + s * kKeysS, k_lo + (uint32_t)(ks * 32 >> 4), k_hi, (uint32_t)q_desc0 + (uint32_t)(ks * 32 >> 4), q_hi, idesc,
+                             ks ? 1u : 0u);
+    };
+    auto pv_keys = [&](uint32_t issue, uint32_t s, uint32_t rows, uint32_t accumulate) {
+        const uint32_t v_lo = (uint32_t)v_desc0 + (v_seq % kFp8VSlots) * (uint32_t)(kSlotBytes >> 4);
+        const uint32_t p_lo = (uint32_t)p_desc0 + s * (uint32_t)(kPBytes >> 4), p_hi = (uint32_t)(p_desc0 >> 32);
+        const uint32_t idesc = umma_idesc_16bit(128, 0, 1, 1, true) | rows >> 3 << 17;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+            umma_ss_lh_if(issue, tmem + kKeysO + s * 64, v_lo + (uint32_t)(ks * 4096 >> 4), v_hi, p_lo + (uint32_t)(ks * 2048 >> 4), p_hi, idesc,
+                          ks ? 1u : accumulate);
+    };
+    auto next_k = [&] { if (++k_place == kPlaces) { k_place = 0; k_parity ^= 1u; } };
+
+    for (;;) {
+        meet_before_segment(aux, seg_no, false);
+        const Segment g = announced_segment(aux, seg_no);
+        const int tile0 = __reduce_max_sync(kAll, g.tile0), tile1 = __reduce_max_sync(kAll, g.tile1);
+        if (tile1 == 0) break;
+        const bool shared = kWide && __reduce_max_sync(kAll, g.shared ? 1 : 0) != 0;
+        const int p_threads = kWide ? 160 : 32 + 32 * __reduce_max_sync(kAll, live_warps_fp8(g.M));
+        const uint32_t keys = (uint32_t)__reduce_max_sync(kAll, keys_rows(g.M));      // keys on lanes: the padded rows
+        bool ok = __all_sync(kAll, mbar_wait(smem_u32(&aux->q_full), seg_no & 1u, abort_flag));
+        const int T = tile1 - tile0;
+        const int n_it[2] = {shared ? T : (T + 1) >> 1, shared ? T : T >> 1};
+#pragma unroll 1
+        for (int i = -1; i < n_it[0]; ++i) {
+            if (kWide && shared && ok && i >= 0 && i + 1 < T) {      // the middle of a 256-row unit: a turn without conditions
+                const uint32_t acc0 = i > 0 ? 1u : 0u;
+                uint32_t q_lo = (uint32_t)q_desc0, tS = tmem, s_bar = s_full;
+                const uint32_t v_bar = v_empty + (v_seq % kFp8VSlots) * 8u, k_bar = raw_empty + k_place * 16u;
+#pragma unroll 1
+                for (uint32_t s = 0; s < 2; ++s) {
+                    asm volatile("bar.sync %0, 160;" ::"r"(4 + s) : "memory");
+                    tc_fence_after();
+                    pv(elected, tS, acc0);
+                    umma_commit_if(s ? elected : 0u, v_bar);
+                    if (s == 0) asm volatile("bar.sync 6, 64;" ::: "memory");
+                    qk(elected, tS, q_lo);
+                    umma_commit_if(elected, s_bar);
+                    umma_commit_if(s ? elected : 0u, k_bar);
+                    tS += 128; q_lo += (uint32_t)(kPieces<kF16> * kPieceBytes >> 4); s_bar += 8;
+                }
+                next_k();
+                ++v_seq;
+                continue;
+            }
+            if (!shared && ok && i >= 0 && i + 1 < n_it[1]) {        // of another unit: both streams have both products
+#pragma unroll 1
+                for (uint32_t s = 0; s < 2; ++s) {
+                    const uint32_t tS = tmem + s * 128;
+                    asm volatile("bar.sync %0, %1;" ::"r"(4 + s), "r"(p_threads) : "memory");
+                    tc_fence_after();
+                    if (keys) pv_keys(elected, s, keys, i > 0 ? 1u : 0u);
+                    else pv(elected, tS, i > 0 ? 1u : 0u);
+                    umma_commit_if(elected, v_empty + (v_seq % kFp8VSlots) * 8u);
+                    ++v_seq;
+                    if (keys) qk_keys(elected, s, keys);
+                    else qk(elected, tS, (uint32_t)q_desc0);
+                    umma_commit_if(elected, s_full + s * 8u);
+                    umma_commit_if(elected, raw_empty + k_place * 16u);
+                    next_k();
+                }
+                continue;
+            }
+#pragma unroll 1
+            for (uint32_t s = 0; s < 2; ++s) {
+                const int n_s = s ? n_it[1] : n_it[0];
+                const bool do_pv = i >= 0 && i < n_s, do_qk = i + 1 < n_s;
+                const bool last_reader = !shared || s == 1;
+                const uint32_t tS = tmem + s * 128;
+                if (do_pv) {
+                    // P of tile i is announced on hardware barrier 4 + s (and with it V of the tile and, but for 256-row units, the stream's
+                    // next K)
+                    asm volatile("bar.sync %0, %1;" ::"r"(4 + s), "r"(p_threads) : "memory");
+                    tc_fence_after();
+                    const uint32_t issue = ok ? elected : 0u;
+                    if (keys) pv_keys(issue, s, keys, i > 0 ? 1u : 0u);
+                    else pv(issue, tS, i > 0 ? 1u : 0u);
+                    // only the segment end waits for it; made on every path, like the announcement of S below
+                    umma_commit_if(i == n_s - 1 ? issue : 0u, o_done + s * 8u);
+                    if (!ok && i == n_s - 1 && elected) mbar_arrive(o_done + s * 8u);
+                    umma_commit_if(last_reader ? issue : 0u, v_empty + (v_seq % kFp8VSlots) * 8u);
+                    if (last_reader) ++v_seq;
+                }
+                if (do_qk) {
+                    if (i >= 0) {
+                        if (shared && s == 0) asm volatile("bar.sync 6, 64;" ::: "memory");
+                    } else if (!(shared && s == 1)) {
+                        ok = __all_sync(kAll, mbar_wait(raw_full + k_place * 16u, k_parity, abort_flag)) && ok;
+                    }
+                    tc_fence_after();
+                    const uint32_t issue = ok ? elected : 0u;
+                    if (keys) qk_keys(issue, s, keys);
+                    else qk(issue, tS, (uint32_t)q_desc0 + ((shared && s) ? (uint32_t)(kPieces<kF16> * kPieceBytes >> 4) : 0u));
+                    // S is announced on every path (mma_loop says why)
+                    umma_commit_if(issue, s_full + s * 8u);
+                    if (!ok && elected) mbar_arrive(s_full + s * 8u);
+                    umma_commit_if(last_reader ? issue : 0u, raw_empty + k_place * 16u);
+                    if (last_reader) next_k();
+                }
             }
         }
+        ++seg_no;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ softmax warpgroups
+// Q rows to e4m3 pieces in shared memory, rows of 128 bytes (K-major, 128-byte swizzle); rows beyond M are zeros.  A thread has eight elements
+// (piece `c` of sixteen) of every eighth row, `count` rows from packed row `row` on; `dst`: the row's place in the first piece, the
+// next piece's lies `piece_bytes` on.
+template <bool kF16>
+__device__ __forceinline__ void load_q_fp8(const AttnParams& p, const Segment& g, AuxFp8* aux, unsigned char* dst, const int piece_bytes, int row,
+                                           const int count, const int c) {
+    const int G = p.group;
+    dst += ((c >> 1) ^ (row & 7)) * 16 + (c & 1) * 8;
+#pragma unroll 1
+    for (int j0 = 0; j0 < count; j0 += 4) {
+        uint4 u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const unsigned r = (unsigned)(row + 8 * j), node = row_node(p, r);
+            const __nv_bfloat16* src = p.q + ((long long)(g.node_base + node) * p.num_q_heads + g.h * G + (r - node * G)) * kHeadDim + c * 8;
+            u[j] = j0 + j < count && r < (unsigned)g.M ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j0 + j >= count) break;
+            const uint32_t w[4] = {u[j].x, u[j].y, u[j].z, u[j].w};
+            float x[8];
+            uint32_t most = 0u;                        // bits of the largest magnitude; a NaN's are larger than any
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (kF16) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                    x[2 * i] = f.x; x[2 * i + 1] = f.y;
+                } else {
+                    x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+                }
+                most = max(most, max(__float_as_uint(x[2 * i]) & 0x7fffffffu, __float_as_uint(x[2 * i + 1]) & 0x7fffffffu));
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+            // the smallest power of two with (largest magnitude) <= 448 of them (block_exponent, over fp32's range)
+            const int e = max(-110, min(110, (int)((most + 0x1fffffu) >> 23) - 135));
+            const float inv = exp2_int(-e);
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = x[i] * inv;
+#pragma unroll
+            for (int piece = 0; piece < kPieces<kF16>; ++piece) {
+                const uint2 v = make_uint2(pack_e4m3x4(y[0], y[1], y[2], y[3]), pack_e4m3x4(y[4], y[5], y[6], y[7]));
+                *reinterpret_cast<uint2*>(dst + piece * piece_bytes) = v;
+                if (piece + 1 < kPieces<kF16>) {
+                    const float4 a = e4m3x4_to_f32(v.x), b = e4m3x4_to_f32(v.y);
+                    y[0] -= a.x; y[1] -= a.y; y[2] -= a.z; y[3] -= a.w; y[4] -= b.x; y[5] -= b.y; y[6] -= b.z; y[7] -= b.w;
+                }
+            }
+            // (a row with an infinity or a NaN has no pieces: its scores are NaN, and so is what comes of them)
+            if (c == 0) aux->row_scale[row + 8 * j] = most >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2_int(e);
+            dst += 1024;
+        }
+        row += 32;
+    }
+}
+
+// Weights are kept 2^7 above exp2(score - m), up to 2^15, so that fp16 (largest 65504, smallest step 2^-24) holds what is 2^-31 of the
+// reference.  The normaliser sums them as they are, not as fp16 rounds them: that is off by at most 2^-12 of the output, where one
+// key has all the weight, and two conversions and an addition per pair of keys less (70B with 32 nodes 647 -> 592 us).
+constexpr float kWeightShift = 7.f;
+constexpr float kWeightLimit = 32768.f;          // 2^(8 + 7)
+// Rows on lanes: the weights of a tile against the running maximum m, 32 columns of S at a time.  False, with nothing stored, if some
+// row's weights show that a score may exceed m by more than the lazy threshold (`force`: this row's do).
+__device__ __forceinline__ bool weigh_tile(const uint32_t tS, const float* kscale, const float scale2, const float m, float& l, bool& force) {
+    const uint64_t neg_m_x2 = pack_f32x2(kWeightShift - m, kWeightShift - m);
+    uint64_t ex_a = 0ull, ex_b = 0ull;
+    uint32_t pk[64];
+    uint32_t buf_a[32], buf_b[32];
+    tmem_ld32(tS, buf_a);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint32_t (&cur)[32] = (c & 1) ? buf_b : buf_a;
+        uint32_t (&nxt)[32] = (c & 1) ? buf_a : buf_b;
+        const float s0 = kscale[2 * c] * scale2, s1 = kscale[2 * c + 1] * scale2;
+        const uint64_t s0_x2 = pack_f32x2(s0, s0), s1_x2 = pack_f32x2(s1, s1);
+        tmem_wait_ld();
+        tmem_loaded(cur);
+        if (c < 3) tmem_ld32(tS + (c + 1) * 32, nxt);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float x0, x1;
+            const uint64_t xx = fma_f32x2(pack_f32x2(__uint_as_float(cur[2 * j]), __uint_as_float(cur[2 * j + 1])), j < 8 ? s0_x2 : s1_x2, neg_m_x2);
+            unpack_f32x2(xx, x0, x1);
+            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+            pk[c * 16 + j] = pack2_16bit<true>(p0, p1);
+            const uint64_t pe = pack_f32x2(p0, p1);
+            if (j & 1) ex_b = add_f32x2(ex_b, pe);
+            else ex_a = add_f32x2(ex_a, pe);
+        }
+    }
+    float b0, b1;
+    unpack_f32x2(add_f32x2(ex_a, ex_b), b0, b1);
+    force = (b0 + b1) > kWeightLimit;
+    if (__any_sync(0xffffffffu, force)) return false;
+    tmem_st32(tS, reinterpret_cast<uint32_t(&)[32]>(pk[0]));
+    tmem_st32(tS + 32, reinterpret_cast<uint32_t(&)[32]>(pk[32]));
+    l += b0 + b1;
+    return true;
+}
+
+// log-sum-exp of a row from its reference and its sum of shifted weights (a NaN sum stays one)
+__device__ __forceinline__ float lse_of_sum(float m, float sum) {
+    return sum > 0.f ? (m - kWeightShift + __log2f(sum)) * 0.6931471805599453f : sum == 0.f ? -INFINITY : sum;
+}
+__device__ __forceinline__ unsigned ordered(float x) {        // sorts like x; a NaN is below everything
+    const unsigned u = __float_as_uint(x);
+    return x != x ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(unsigned u) { return u == 0u ? -INFINITY : __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+__device__ __forceinline__ float min_or_nan(float x, float y) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+// Meets the calling stream's 128 threads; true for all if it is for one.
+__device__ __forceinline__ bool any_of_stream(int s, bool mine) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+                 : "=r"(r) : "r"(7 + s), "r"(mine ? 1u : 0u) : "memory");
+    return r != 0;
+}
+
+// What the products of a stream wait for besides P, looked at before P is announced by two of the warps that announce it: the first waits
+// until V of tile `seq` has been turned into fp16, the second until the stream's next K tile has landed (`next`).  The MMA warp then waits
+// on a hardware barrier alone (25 clocks if it is late; a look at an mbarrier is 100 to 190, and it is the MMA warp whose instructions
+// a tile waits for).  A wait that gives up raises the abort flag; P is announced all the same.
+template <uint32_t kPlaces>
+__device__ __forceinline__ void tiles_for_products(AuxFp8* aux, uint32_t seq, bool next, int wtid, volatile int* abort_flag) {
+    if (wtid < 32) mbar_wait(smem_u32(&aux->v_full[seq % kFp8VSlots]), (seq / kFp8VSlots) & 1u, abort_flag);
+    else if (wtid < 64 && next) mbar_wait(smem_u32(&aux->raw_full[2u * ((seq + 2u) % kPlaces)]), ((seq + 2u) / kPlaces) & 1u, abort_flag);
+    __syncwarp();
+}
+
+// ------------------------------------------------------------------------------------------ keys on lanes
+// A stream's key tiles of one segment.  Thread = key of the tile; kRows = the unit's rows, padded.  A row's numbers (scale, reference) lie in
+// shared memory and are the same for the stream's four warps, which agree after each tile on whether all scores stayed
+// within the lazy threshold of their rows' references.  `sum[r]`: the weights of row r over this thread's keys.
+template <int kRows, bool kF16>
+struct KeysStream {
+    const AttnParams& p;
+    AuxFp8* aux;
+    KeysScratch* k;
+    unsigned char* p_tile;           // this stream's P
+    uint32_t tS, tO;
+    int s, wtid;
+    uint64_t sum[kRows / 2];         // pairs of rows
+
+    __device__ __forceinline__ void begin(const Segment& g) {
+        if (wtid < kRows) {
+            // rows beyond M: weights of 0; others: any score at all is above the threshold until the first reference is there
+            k->scale[s][wtid] = wtid < g.M ? p.sm_scale * 1.4426950408889634f * aux->row_scale[wtid] : 0.f;
+            k->bias[s][wtid] = wtid < g.M ? 1e30f : -INFINITY;
+            k->m[s][wtid] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < kRows / 2; ++r) sum[r] = 0ull;
+        named_barrier(7 + s, 128);
+    }
+    // scores of 16 rows from `r0` on, without their scales: the pieces' columns added up
+    __device__ __forceinline__ void scores(int r0, uint64_t (&x)[8]) {
+        uint32_t a[kPieces<kF16>][16];
+#pragma unroll
+        for (int piece = 0; piece < kPieces<kF16>; ++piece) tmem_ld16(tS + piece * kRows + r0, a[piece]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int piece = 0; piece < kPieces<kF16>; ++piece) {
+            tmem_loaded(a[piece]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint64_t y = pack_f32x2(__uint_as_float(a[piece][2 * j]), __uint_as_float(a[piece][2 * j + 1]));
+                x[j] = piece == 0 ? y : add_f32x2(x[j], y);
+            }
+        }
+    }
+    // The tile reaches drafted positions (or the end of the sequence): what a row does not see gets a score of -inf, in tensor memory.  A slot
+    // past the end may have held a NaN, so all its pieces are replaced.
+    __device__ __forceinline__ void mask(const Segment& g, int t) {
+        const int j = t * kTileKeys + wtid - g.L;              // this key as a drafted node; below 0: context
+#pragma unroll 1
+        for (int r0 = 0; r0 < kRows; r0 += 32) {
+            uint32_t sees = 0u;
+#pragma unroll 1
+            for (int r = 0; r < 32; ++r) {
+                const int row = r0 + r;
+                const bool yes = j < 0 || (row < g.M && j < kMaxNodes && (aux->anc[row_node(p, row)] >> j & 1ull));
+                sees |= yes ? 1u << r : 0u;
+            }
+#pragma unroll 1
+            for (int piece = 0; piece < kPieces<kF16>; ++piece) {
+                uint32_t a[32];
+                tmem_ld32(tS + piece * kRows + r0, a);
+                tmem_wait_ld();
+                tmem_loaded(a);
+#pragma unroll
+                for (int r = 0; r < 32; ++r)
+                    if (!(sees >> r & 1u)) a[r] = piece == 0 ? 0xff800000u : 0u;
+                tmem_st32(tS + piece * kRows + r0, a);
+            }
+        }
+        tmem_wait_st();
+    }
+    // Weights of 32 rows from r0 on against their references, to P and into `sum`; true if some score is above its reference by more than the
+    // threshold.  Weights stop at 2^15.5 (a NaN stays one), so that in that case they can be taken out of `sum` again (kBack; P is
+    // then written anew): what that leaves in it is 2^-24 of a sum that the new reference makes small.
+    template <int r0, bool kBack>
+    __device__ __forceinline__ bool weigh(float kscale) {
+        const uint64_t ks_x2 = pack_f32x2(kscale, kscale);
+        __half2 top = __float2half2_rn(0.f);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint64_t x[8];
+            uint32_t pk[8];
+            scores(r0 + 16 * h, x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const ulonglong2 sc = *reinterpret_cast<const ulonglong2*>(&k->scale[s][r0 + 16 * h + 4 * j]);
+                const ulonglong2 bi = *reinterpret_cast<const ulonglong2*>(&k->bias[s][r0 + 16 * h + 4 * j]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint64_t y = fma_f32x2(mul_f32x2(x[2 * j + i], i ? sc.y : sc.x), ks_x2, i ? bi.y : bi.x);
+                    float y0, y1;
+                    unpack_f32x2(y, y0, y1);
+                    const float p0 = fast_exp2(min_or_nan(y0, 15.5f)), p1 = fast_exp2(min_or_nan(y1, 15.5f));
+                    pk[2 * j + i] = pack2_16bit<true>(p0, p1);
+                    top = __hmax2(top, *reinterpret_cast<const __half2*>(&pk[2 * j + i]));
+                    uint64_t& to = sum[r0 / 2 + 8 * h + 2 * j + i];
+                    to = add_f32x2(to, kBack ? pack_f32x2(-p0, -p1) : pack_f32x2(p0, p1));
+                }
+            }
+            if constexpr (!kBack) {
+                // P: keys' rows of 128 bytes, 16-byte piece c at place c ^ (key & 7); MN-major operand
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    *reinterpret_cast<uint4*>(p_tile + (((r0 / 8 + 2 * h + c) ^ (wtid & 7)) << 4)) = make_uint4(pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
+            }
+        }
+        return __low2float(top) > kWeightLimit || __high2float(top) > kWeightLimit;
+    }
+    // The references of 32 rows move up to the tile's largest scores where those are above them (force) or above the threshold.
+    template <int r0>
+    __device__ __forceinline__ void raise(float kscale, bool force, bool first) {
+        if (wtid < 32) k->most[s][wtid] = 0u;
+        named_barrier(7 + s, 128);
+#pragma unroll 1
+        for (int h = 0; h < 32; h += 16) {
+            uint64_t x[8];
+            scores(r0 + h, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float y[2];
+                unpack_f32x2(x[j], y[0], y[1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const unsigned u = __reduce_max_sync(0xffffffffu, ordered(y[i] * k->scale[s][r0 + h + 2 * j + i] * kscale));
+                    if ((wtid & 31) == 0) atomicMax(&k->most[s][h + 2 * j + i], u);
+                }
+            }
+        }
+        named_barrier(7 + s, 128);
+        bool moved = false;
+        if (wtid < 32) {
+            const int row = r0 + wtid;
+            const float m = k->m[s][row], m_new = fmaxf(m, from_ordered(k->most[s][wtid]));
+            const bool real = k->bias[s][row] > -INFINITY;
+            moved = real && (force || first ? m_new > m : m_new - m > kLazyRescale);
+            k->alpha[s][wtid] = moved ? fast_exp2(m - m_new) : 1.f;
+            if (moved) { k->m[s][row] = m_new; k->bias[s][row] = kWeightShift - m_new; }
+        }
+        if (!any_of_stream(s, moved) || first) return;         // (nothing has been added up yet)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[r0 / 2 + r] = mul_f32x2(sum[r0 / 2 + r], pack_f32x2(k->alpha[s][2 * r], k->alpha[s][2 * r + 1]));
+        // S of this tile is here, and the commit that announced it covers the product before it: O may be touched
+        tc_fence_after();
+#pragma unroll 1
+        for (int h = 0; h < 32; h += 16) {
+            uint32_t o[16];
+            tmem_ld16(tO + r0 + h, o);
+            tmem_wait_ld();
+            tmem_loaded(o);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * k->alpha[s][h + r]);
+            tmem_st16(tO + r0 + h, o);
+        }
+        tmem_wait_st();
+    }
+    template <int r0>
+    __device__ __forceinline__ void rows32(float kscale, bool first) {
+        bool force = false;
+        if (!first) {
+            force = any_of_stream(s, weigh<r0, false>(kscale));
+            if (!force) return;
+            weigh<r0, true>(kscale);
+        }
+        raise<r0>(kscale, force, first);
+        weigh<r0, false>(kscale);
+    }
+    // the sums over the stream's keys: lane i of each warp leaves row i's (then row 32 + i's) over the warp
+    __device__ __forceinline__ void finish() {
+        const int lane = wtid & 31, warp = wtid >> 5;
+#pragma unroll
+        for (int r0 = 0; r0 < kRows; r0 += 32) {
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) unpack_f32x2(sum[r0 / 2 + i], v[2 * i], v[2 * i + 1]);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < o; ++i) {
+                    const bool up = lane & o;
+                    const float send = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+                    v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                }
+            k->sum[s][warp][r0 + lane] = v[0];
+        }
+    }
+};
+
+// The key loop and the results of a segment with keys on lanes; `it`, `tile_base`: the stream's S tiles and the CTA's key tiles so far.
+template <int kRows, bool kWide, bool kF16>
+__device__ __forceinline__ void keys_segment(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s, const Segment& g,
+                                             const uint32_t it, const uint32_t od_phase, const uint32_t tile_base, const uint32_t seg_no, const bool leader) {
+    const int wtid = threadIdx.x - 128 - s * 128;
+    volatile int* abort_flag = &aux->abort_flag;
+    const uint32_t lane_sel = (uint32_t)(((threadIdx.x >> 5) & 3) * 32) << 16;
+    constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
+    KeysScratch* k = reinterpret_cast<KeysScratch*>(smem + kScratchOff<kWide, kF16>);
+    const int n_it = g.iters(s);
+    {
+        KeysStream<kRows, kF16> ks{p, aux, k, smem + kPOff<kF16> + s * kPBytes + wtid * 128, tmem + lane_sel + s * kKeysS,
+                                   tmem + lane_sel + kKeysO + s * 64, s, wtid, {}};
+        ks.begin(g);
+        for (int i = 0; i < n_it; ++i) {
+            const int t = g.tile(s, i);
+            mbar_wait_certain(smem_u32(&aux->s_full[s]), (it + i) & 1u, abort_flag);
+            tc_fence_after();
+            const float kscale = aux->note[(tile_base + (uint32_t)(t - g.tile0)) % kNotes].kscale[wtid >> 4];
+            if ((t + 1) * kTileKeys > g.L) ks.mask(g, t);
+            ks.template rows32<0>(kscale, i == 0);
+            if constexpr (kRows == 64) ks.template rows32<32>(kscale, i == 0);
+            tiles_for_products<kPlaces>(aux, tile_base + (uint32_t)(t - g.tile0), i + 1 < n_it, wtid, abort_flag);
+            fence_proxy_async_smem();                  // P is read by the product
+            tc_fence_before();
+            asm volatile("bar.arrive %0, 160;" ::"r"(4 + s) : "memory");      // hand-off of P, once per tile on every path
+        }
+        ks.finish();
+    }
+    if (n_it > 0) mbar_wait_certain(smem_u32(&aux->o_done[s]), od_phase & 1u, abort_flag);
+    tc_fence_after();
+    meet_before_segment(aux, seg_no + 1, leader);    // both streams done: all MMAs of the segment have completed
+    const volatile Segment& again = aux->seg[seg_no % kSegs];
+    const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
+    const bool write_ok = !bad && !*abort_flag;
+    const long long part_base = (2ll * blockIdx.x + (seg_no > 0 ? 1 : 0)) * kRowsOfPartial;
+    const int M = again.M, node_base = again.node_base, h = again.h, G = p.group;
+    const bool whole = again.tile0 == 0 && again.tile1 == again.tiles;
+    const bool use_b = g.iters(1) > 0;
+    tc_fence_after();
+    auto out_row_of = [&](int row) {
+        const int node = (int)row_node(p, row);
+        return (long long)(node_base + node) * p.num_q_heads + h * G + (row - node * G);
+    };
+    if (s == 0 && wtid < kRows) {
+        const int row = wtid;
+        float l[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) l[b] = (k->sum[b][0][row] + k->sum[b][1][row]) + (k->sum[b][2][row] + k->sum[b][3][row]);
+        const float m0 = k->m[0][row], m1 = k->m[1][row], mm = fmaxf(m0, m1);
+        const float a0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - mm), a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mm);
+        const float lt = a0 * l[0] + a1 * l[1], inv = lt > 0.f ? 1.f / lt : 0.f;
+        k->w[0][row] = a0 * inv;
+        k->w[1][row] = a1 * inv;
+        if (row < M) {
+            if (write_ok) {
+                const float lse = lse_of_sum(mm, lt);
+                if (!whole) p.part_lse[part_base + row] = lse;
+                else if (p.lse) p.lse[out_row_of(row)] = lse;
+            } else if (bad && !whole) {
+                p.part_lse[part_base + row] = __uint_as_float(kBadPartial);      // the merge leaves the row alone
+            }
+        }
+    }
+    named_barrier(1, 256);
+    // Lane = channel.  Each warpgroup writes 16 rows of every 32, and a warp's 32 channels of a row are neighbours.
+#pragma unroll 1
+    for (int r0 = 16 * s; r0 < kRows; r0 += 32) {
+        uint32_t oa[16], ob[16];
+        tmem_ld16(tmem + lane_sel + kKeysO + r0, oa);
+        if (use_b) tmem_ld16(tmem + lane_sel + kKeysO + 64 + r0, ob);
+        tmem_wait_ld();
+        tmem_loaded(oa);
+        tmem_loaded(ob);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = r0 + r;
+            float v = __uint_as_float(oa[r]) * k->w[0][row];
+            if (use_b) v = fmaf(__uint_as_float(ob[r]), k->w[1][row], v);
+            if (!write_ok || row >= M) continue;
+            if (whole) {
+                const uint32_t u = pack2_16bit<kF16>(v, 0.f);
+                reinterpret_cast<uint16_t*>(p.out)[out_row_of(row) * kHeadDim + wtid] = (uint16_t)u;
+            } else {
+                // a partial: [32 groups of four channels][rows][4]
+                p.part_o[(part_base * 32 + (long long)(wtid >> 2) * kRowsOfPartial + row) * 4 + (wtid & 3)] = v;
+            }
+        }
+    }
+}
+
+template <bool kWide, bool kF16>
+__device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s /*stream*/) {
+    constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
+    const int wtid = threadIdx.x - 128 - s * 128;          // 0..127 inside the warpgroup; TMEM lane
+    volatile int* abort_flag = &aux->abort_flag;
+    const uint32_t lane_sel = (uint32_t)(((threadIdx.x >> 5) & 3) * 32) << 16;
+    const uint32_t tS = tmem + lane_sel + s * 128;
+    const int G = p.group;
+    uint32_t it = 0, seg_no = 0, od_phase = 0;   // od_phase: segments of this stream that issued a product
+    uint32_t tile_base = 0;                      // key tiles of the CTA's earlier segments
+
+    const bool leader = s == 0 && wtid < 32;
+    meet_before_segment(aux, 0, leader);
+    for (;;) {
+        const Segment g = announced_segment(aux, seg_no);
+        if (g.tile1 == 0) break;
+        const int keys = keys_rows(g.M);         // keys on lanes: the padded rows
+        int parent_i = -1;
+        if (s == 0 && wtid < g.n) parent_i = p.tree_parent[g.node_base + wtid];
+        if (seg_no > 0) named_barrier(1, 256);   // the other warpgroup may still be reading its staging area in the Q block
+        if (leader) const_cast<volatile int&>(aux->seg_reached) = (int)seg_no;
+        {
+            // rows on lanes, 256 rows: a block of 128 rows for each warpgroup; else each loads half of the rows
+            const int half = keys ? keys >> 1 : 64, r_in_8 = wtid >> 4;
+            const int first = g.shared ? r_in_8 : half * s + r_in_8;
+            load_q_fp8<kF16>(p, g, aux, smem + (g.shared ? s * kPieces<kF16> * kPieceBytes : 0) + first * 128, keys ? keys * 128 : kPieceBytes,
+                             (g.shared ? 128 * s : 0) + first, g.shared ? 16 : half >> 3, wtid & 15);
+        }
+        if (s == 0) {
+            if (wtid == 0) aux->seg_bad_tree = 0;
+            named_barrier(2, 128);
+            if (wtid < g.n) {
+                const bool bad = (wtid == 0 && parent_i != -1) || (wtid > 0 && (parent_i < 0 || parent_i >= wtid));
+                if (bad) {
+                    atomicExch(&aux->seg_bad_tree, 1);
+                    report(p.status, kErrBadTree);
+                }
+                aux->parent[wtid] = bad ? (short)-1 : (short)parent_i;
+            }
+            named_barrier(2, 128);
+            if (wtid < g.n) {
+                unsigned long long m = 0;
+                if (!aux->seg_bad_tree)
+                    for (int j = wtid, guard = 0; j >= 0 && guard < kMaxNodes; j = aux->parent[j], ++guard) m |= 1ull << j;
+                aux->anc[wtid] = m;
+            }
+        }
+        fence_proxy_async_smem();
+        named_barrier(1, 256);                 // masks and the tree verdict are visible to both warpgroups
+        mbar_arrive(smem_u32(&aux->q_full));
+
+        const int n_it = g.iters(s);
+        if (keys) {
+            if (keys == 32) keys_segment<32, kWide, kF16>(p, aux, smem, tmem, s, g, it, od_phase, tile_base, seg_no, leader);
+            else keys_segment<64, kWide, kF16>(p, aux, smem, tmem, s, g, it, od_phase, tile_base, seg_no, leader);
+            it += (uint32_t)n_it;
+            if (n_it > 0) ++od_phase;
+            tc_fence_before();
+            tile_base += (uint32_t)(g.tile1 - g.tile0);
+            ++seg_no;
+            continue;
+        }
+        const int rr = (g.shared ? s * 128 : 0) + wtid;            // packed row of this thread
+        const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
+        const float scale2 = p.sm_scale * 1.4426950408889634f * aux->row_scale[rr];
+        const int live = kWide ? 4 : live_warps_fp8(g.M);
+        const bool idle = (wtid >> 5) >= live;       // no row of the unit in this warp: straight to the segment's end
+        float m = -INFINITY, l = 0.f;
+
+        for (int i = 0; i < (idle ? 0 : n_it); ++i) {
+            const int t = g.tile(s, i);
+            mbar_wait_certain(smem_u32(&aux->s_full[s]), (it + i) & 1u, abort_flag);
+            tc_fence_after();
+            const float* kscale = aux->note[(tile_base + (uint32_t)(t - g.tile0)) % kNotes].kscale;
+            if ((t + 1) * kTileKeys > g.L) {
+                // The tile reaches drafted positions (or the end of the sequence): at most two tiles per unit.
+                // Visibility of its 128 keys for this row: prefix keys all, drafted key j iff ancestor-or-self.
+                // The mask is applied to S in tensor memory, 32 columns at a time, before the common path reads it.
+                const int j0 = t * kTileKeys - g.L;
+                unsigned long long lo, hi;
+                if (j0 >= 0) {
+                    lo = j0 < 64 ? anc_row >> j0 : 0ull;
+                    hi = 0ull;
+                } else {
+                    const int k = -j0;   // 1..127 prefix keys at the front of the tile
+                    if (k >= 64) { lo = ~0ull; hi = (k == 64 ? 0ull : (~0ull >> (128 - k))) | (anc_row << (k - 64)); }
+                    else { lo = (~0ull >> (64 - k)) | (anc_row << k); hi = anc_row >> (64 - k); }
+                }
+#pragma unroll 1
+                for (int c4 = 0; c4 < 4; ++c4) {
+                    const uint32_t bits = (uint32_t)((c4 < 2 ? lo : hi) >> ((c4 & 1) * 32));
+                    uint32_t r[32];
+                    tmem_ld32(tS + c4 * 32, r);
+                    tmem_wait_ld();
+                    tmem_loaded(r);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (!((bits >> j) & 1u)) r[j] = 0xff800000u;   // -inf
+                    tmem_st32(tS + c4 * 32, r);
+                }
+                tmem_wait_st();
+            }
+            bool done = false, force = false;
+            if (i > 0 && !__any_sync(0xffffffffu, m == -INFINITY)) {
+                done = weigh_tile(tS, kscale, scale2, m, l, force);
+            }
+            if (!done) {
+                // The long way: the tile's maximum first, then the weights; twice over tensor memory and rolled, because
+                // it runs on a segment's first tile and after a jump of the maximum only.
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int c4 = 0; c4 < 4; ++c4) {
+                    uint32_t r[32];
+                    tmem_ld32(tS + c4 * 32, r);
+                    tmem_wait_ld();
+                    tmem_loaded(r);
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        float a = __uint_as_float(r[16 * hf]);
+#pragma unroll
+                        for (int j = 1; j < 16; ++j) a = fmaxf(a, __uint_as_float(r[16 * hf + j]));
+                        mx = fmaxf(mx, a * (kscale[2 * c4 + hf] * scale2));
+                    }
+                }
+                const float m_new = fmaxf(m, mx);
+                // (false when both are -inf: NaN compares false)  A tile sent here by the fast path's sum moves m up at once.
+                const bool need = force ? m_new > m : (m_new - m) > kLazyRescale;
+                if (__any_sync(0xffffffffu, need)) {
+                    const float alpha = (m_new == -INFINITY) ? 1.f : fast_exp2(m - m_new);
+                    if (i > 0) {
+                        // S of this tile is here, and its product was issued after O += P V of the tile before: the
+                        // commit that announced S covers that product too, so O may be touched now
+                        tc_fence_after();
+                        const uint32_t tO = tmem + lane_sel + 256 + s * 128;
+#pragma unroll 1
+                        for (int c4 = 0; c4 < 4; ++c4) {
+                            uint32_t o[32];
+                            tmem_ld32(tO + c4 * 32, o);
+                            tmem_wait_ld();
+                            tmem_loaded(o);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                            tmem_st32(tO + c4 * 32, o);
+                        }
+                        tmem_wait_st();
+                        l *= alpha;
+                    }
+                    m = m_new;
+                }
+                const float neg_m = (m == -INFINITY) ? 0.f : kWeightShift - m;
+                float sum = 0.f;
+#pragma unroll 1
+                for (int c4 = 0; c4 < 4; ++c4) {
+                    // the weights of 32 keys take columns that hold only scores already read (16 c4 + 16 <= 32 (c4 + 1))
+                    uint32_t sv[32], pk[16];
+                    tmem_ld32(tS + c4 * 32, sv);
+                    tmem_wait_ld();
+                    tmem_loaded(sv);
+                    float x_a = 0.f, x_b = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float sc = kscale[2 * c4 + (j >> 3)] * scale2;
+                        const float p0 = fast_exp2(fmaf(__uint_as_float(sv[2 * j]), sc, neg_m)), p1 = fast_exp2(fmaf(__uint_as_float(sv[2 * j + 1]), sc, neg_m));
+                        pk[j] = pack2_16bit<true>(p0, p1);
+                        x_a += p0; x_b += p1;
+                    }
+                    tmem_st16(tS + c4 * 16, pk);
+                    sum += x_a + x_b;
+                }
+                l += sum;
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            // (both streams on one tile: stream 1's product follows stream 0's)
+            if (!g.shared) tiles_for_products<kPlaces>(aux, tile_base + (uint32_t)(t - g.tile0), i + 1 < n_it, wtid, abort_flag);
+            else if (kWide && s == 0) tiles_for_products<kPlaces>(aux, tile_base + (uint32_t)i, false, wtid, abort_flag);
+            // Hand-off of P on hardware barrier 4 + s, once per key tile of this stream, on every path (softmax_loop)
+            asm volatile("bar.arrive %0, %1;" ::"r"(4 + s), "r"(32 * live + 32) : "memory");
+            // Units of more than 128 rows: the next K tile has landed (hardware barrier 6, T - 1 times; softmax_loop)
+            if (kWide && g.shared && s == 0 && wtid < 32 && i + 1 < n_it) {
+                const uint32_t seq = tile_base + (uint32_t)(i + 1);
+                mbar_wait(smem_u32(&aux->raw_full[2u * (seq % kPlaces)]), (seq / kPlaces) & 1u, abort_flag);
+                __syncwarp();
+                asm volatile("bar.arrive 6, 64;" ::: "memory");
+            }
+        }
+        it += (uint32_t)n_it;
+
+        // ---- segment end: every product of this stream has completed
+        // (an idle warp sleeps on the hardware barrier below instead; it touches no tensor memory)
+        if (n_it > 0) {
+            if (!idle) mbar_wait_certain(smem_u32(&aux->o_done[s]), od_phase & 1u, abort_flag);
+            ++od_phase;
+        }
+        tc_fence_after();
+        // both streams on the same rows: they exchange (m, l) through the first columns of their S (softmax_loop)
+        if (!g.shared && !idle) {
+            const uint32_t mine[4] = {__float_as_uint(m), __float_as_uint(l), 0u, 0u};
+            tmem_st4(tS, mine);
+            tmem_wait_st();
+            tc_fence_before();
+        }
+        meet_before_segment(aux, seg_no + 1, leader);    // both streams done: all MMAs of the segment have completed
+        const volatile Segment& again = aux->seg[seg_no % kSegs];
+        const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
+        const bool write_ok = !bad && !*abort_flag;
+        // only the first and the last unit of a CTA's piece can be cut: two partial slots per CTA
+        const long long part_base = (2ll * blockIdx.x + (seg_no > 0 ? 1 : 0)) * kRows;
+        const int M = again.M, node_base = again.node_base, h = again.h;
+        auto out_row_of = [&](int row) {
+            const int node = (int)row_node(p, row);
+            return (long long)(node_base + node) * p.num_q_heads + h * G + (row - node * G);
+        };
+        const bool row_ok = write_ok && rr < M;
+        const bool whole = again.tile0 == 0 && again.tile1 == again.tiles;
+        // staging for coalesced stores: Q is idle now (every MMA of the segment is done)
+        float* stage = reinterpret_cast<float*>(smem + (s * 4 + ((threadIdx.x >> 5) & 3)) * kStageBytesPerWarp);
+        // a partial: [32 groups of four channels][kRows rows][4]
+        float4* part_o = reinterpret_cast<float4*>(p.part_o) + part_base * 32;
+        float wa, wb = 0.f, lse;
+        uint32_t tOa = tmem + lane_sel + 256 + s * 128, tOb = tmem + lane_sel + 384;
+        bool use_b = false, write_lse = true;
+        int c_first = 0, c_count = 4;
+        if (g.shared) {
+            wa = l > 0.f ? 1.f / l : 0.f;
+            lse = lse_of_sum(m, l);
+        } else {
+            // (a stream without a tile has m = -inf and nothing in its sums)
+            use_b = g.iters(1) > 0;
+            float m0 = m, l0 = l, m1 = m, l1 = l;
+            uint32_t st[4];
+            tc_fence_after();
+            if (!idle && (kWide || s == 1)) {
+                tmem_ld4(tmem + lane_sel, st);
+                tmem_wait_ld();
+                tmem_loaded(st);
+                m0 = __uint_as_float(st[0]); l0 = __uint_as_float(st[1]);
+            }
+            if (!idle && (kWide || s == 0)) {
+                tmem_ld4(tmem + lane_sel + 128, st);
+                tmem_wait_ld();
+                tmem_loaded(st);
+                m1 = __uint_as_float(st[0]); l1 = __uint_as_float(st[1]);
+            }
+            const float mm = fmaxf(m0, m1);
+            const float a0 = (m0 == -INFINITY) ? 0.f : fast_exp2(m0 - mm);
+            const float a1 = (m1 == -INFINITY) ? 0.f : fast_exp2(m1 - mm);
+            const float lt = a0 * l0 + a1 * l1;
+            const float inv = lt > 0.f ? 1.f / lt : 0.f;
+            wa = a0 * inv; wb = a1 * inv;
+            lse = lse_of_sum(mm, lt);
+            tOa = tmem + lane_sel + 256;
+            write_lse = s == 0;
+            c_first = 2 * s; c_count = 2;
+        }
+        if (idle) c_count = 0;
+#pragma unroll 1
+        for (int c4 = c_first; c4 < c_first + c_count; ++c4) {
+            uint32_t oa[32], ob[32];
+            tmem_ld32(tOa + c4 * 32, oa);
+            if (use_b) tmem_ld32(tOb + c4 * 32, ob);
+            tmem_wait_ld();
+            tmem_loaded(oa);
+            tmem_loaded(ob);
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                v[j] = __uint_as_float(oa[j]) * wa;           // rows that saw no key have O = 0 and weight 0
+                if (use_b) v[j] = fmaf(__uint_as_float(ob[j]), wb, v[j]);
+            }
+            if (whole) {
+                store_rows32<kF16>(p, stage, rr < M ? out_row_of(rr) : 0, row_ok, c4 * 32, v);
+            } else if (row_ok) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    part_o[(c4 * 8 + j) * kRows + rr] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            }
+        }
+        if (row_ok && write_lse) {
+            if (whole) { if (p.lse) p.lse[out_row_of(rr)] = lse; }
+            else p.part_lse[part_base + rr] = lse;
+        } else if (bad && write_lse && !whole && rr < M) {
+            p.part_lse[part_base + rr] = __uint_as_float(kBadPartial);      // the merge leaves the row alone
+        }
+        tc_fence_before();
+        tile_base += (uint32_t)(g.tile1 - g.tile0);
+        ++seg_no;
     }
 }
 
@@ -187,13 +1101,14 @@ verify_attn_fp8_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k
         return;
     }
     if (tid == 0) {
-        for (int i = 0; i < kFp8Slots; ++i) {
-            mbar_init(smem_u32(&aux->empty[i]), 1);
-            mbar_init(smem_u32(&aux->full16[i]), 4);
-        }
-        for (int i = 0; i < kRawSlots<kWide>; ++i) {
-            mbar_init(smem_u32(&aux->raw_full[i]), i & 1 ? 1 : 2);      // the bytes, and for a tile's K slot the note
-            mbar_init(smem_u32(&aux->raw_empty[i]), 4);
+        for (int i = 0; i < kRawTiles<kWide, kF16>; ++i)
+            for (int kv = 0; kv < 2; ++kv) {
+                mbar_init(smem_u32(&aux->raw_full[2 * i + kv]), 2);            // the bytes and the note
+                mbar_init(smem_u32(&aux->raw_empty[2 * i + kv]), kv ? 4 : 1);  // V: the converting warps; K: the products
+            }
+        for (int i = 0; i < kFp8VSlots; ++i) {
+            mbar_init(smem_u32(&aux->v_full[i]), 4);
+            mbar_init(smem_u32(&aux->v_empty[i]), 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&aux->s_full[s]), 1);
@@ -239,18 +1154,18 @@ verify_attn_fp8_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k
         if (!kManySeqs) wait_for_inputs();
         if (warp == 0) {
             if constexpr (!kManySeqs) build_walk_small(p, w);
-            producer_loop_fp8<kWide, kManySeqs>(p, &kmap, &vmap, aux, smem_base + kRawOff<kWide>, w);
+            producer_loop_fp8<kWide, kF16, kManySeqs>(p, &kmap, &vmap, aux, smem_base + kRawOff<kWide, kF16>, w);
         } else if (warp == 1) {
-            mma_loop<kWide, true, true>(aux, smem_base, tmem);
+            mma_loop_fp8<kWide, kF16>(aux, smem_base, tmem);
         }
     } else if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         if (!kManySeqs) wait_for_inputs();
-        convert_loop<kWide>(p, aux, smem);
+        convert_loop<kWide, kF16>(p, aux, smem);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         if (!kManySeqs) wait_for_inputs();
-        softmax_loop<kWide, kF16, true>(p, aux, smem, tmem, warp >= 8 ? 1 : 0);
+        softmax_loop_fp8<kWide, kF16>(p, aux, smem, tmem, warp >= 8 ? 1 : 0);
     }
 
     tc_fence_before();

@@ -108,7 +108,7 @@ struct Aux {
     Segment seg[kSegs];
     int sched_b0;
     long long sched_tile_begin;
-    long long scan_tiles[16];
+    long long scan_tiles[16];        // one place per warp of a CTA (16 in verify_attn_fp8.cuh)
     long long total_tiles;
     int scan_units[16];
     int scan_tmin[16], scan_tmax[16];
@@ -116,36 +116,6 @@ struct Aux {
     unsigned long long anc[kMaxNodes];
 };
 static_assert(sizeof(Aux) <= kAuxBytes, "aux area too small");
-
-// The 8-bit cache (kFp8, verify_attn_fp8.cuh): four more warps turn the tiles that TMA brings into fp16 tiles in a ring of four slots, which
-// lies where the ring of the 16-bit instances lies; the roles here read that one.  Both products are fp16 ones whatever q's type.
-constexpr int kFp8Slots = 4;
-constexpr int kFp8Places = kFp8Slots / 2;        // tiles: a K and a V slot each
-constexpr int kFp8RawSlots = 4;                  // of 16 KB, beside one block of Q rows (two beside two)
-struct TileNote {                                // what the converting warps have to know of a tile besides its bytes
-    int valid;                                   // keys of the sequence in it; -1: no more tiles
-    int8_t exp[2][kTileKeys / 16];               // exponents of its pages, K and V
-};
-struct AuxFp8 : Aux {
-    uint64_t raw_full[kFp8RawSlots], raw_empty[kFp8RawSlots];
-    uint64_t full16[kFp8Slots];                  // the fp16 slots' arrivals, one from each converting warp
-    TileNote note[kFp8RawSlots / 2];
-    float row_scale[kRows];                      // what the rows of Q were divided by (a power of two)
-};
-static_assert(sizeof(AuxFp8) <= kAuxBytes, "aux area too small");
-template <bool kWide, bool kFp8> constexpr int kOperandSlots = kFp8 ? kFp8Slots : kRingSlots<kWide>;
-
-// The barrier on which the K (kv = 0) or V tile of the CTA's key tile `seq` arrives, and whether it has.
-template <bool kFp8>
-__device__ __forceinline__ bool wait_for_tile(Aux* aux, uint32_t seq, int kv, volatile int* abort_flag) {
-    if constexpr (kFp8)
-        return mbar_wait(smem_u32(&static_cast<AuxFp8*>(aux)->full16[2u * (seq % kFp8Places) + kv]), (seq / kFp8Places) & 1u, abort_flag);
-    else       // (one barrier for both)
-        return mbar_wait(smem_u32(&aux->full[seq % kTilesInFlight]), (seq / kTilesInFlight) & 1u, abort_flag);
-}
-// With fp16 weights of any row of Q the lazy reference may lie 2^8 below a score; weights are kept 2^7 above that, up to 2^15, so that fp16
-// (largest 65504, smallest step 2^-24) holds what is 2^-31 of the reference.
-template <bool kFp8> constexpr float kWeightShift = kFp8 ? 7.f : 0.f;
 
 // Walks the CTA's piece [t, t_end) of the line unit by unit.  The producer warp does, one segment after the other, and
 // announces each to the other roles in shared memory: with a walker and the schedule's arithmetic in every role the
@@ -416,10 +386,9 @@ __device__ __forceinline__ void producer_loop(const AttnParams& p, const CUtenso
 //    one on which stream 0's warpgroup tells that it has seen the next key tile arrive (units of up to 128 rows
 //    wait for the tile itself);
 //  * one turn's text serves both streams and all tiles.
-template <bool kWide, bool kF16, bool kFp8 = false>
+template <bool kWide, bool kF16>
 __device__ __forceinline__ void mma_loop(Aux* aux, uint32_t smem_base, uint32_t tmem) {
     constexpr unsigned kAll = 0xffffffffu;
-    constexpr int kSlots = kOperandSlots<kWide, kFp8>;
     volatile int* abort_flag = &aux->abort_flag;
     constexpr uint32_t idesc_qk = umma_idesc_16bit(128, kTileKeys, 0, 0, kF16);
     constexpr uint32_t idesc_pv = umma_idesc_16bit(128, kHeadDim, 0, 1, kF16);
@@ -444,7 +413,7 @@ __device__ __forceinline__ void mma_loop(Aux* aux, uint32_t smem_base, uint32_t 
         const int n_it[2] = {shared ? T : (T + 1) >> 1, shared ? T : T >> 1};
 
         // ring slots of the V tile and of the K tile that the next turn needs
-        uint32_t k_slot = item_base % kSlots, v_slot = (item_base + 1u) % kSlots;
+        uint32_t k_slot = item_base % kRingSlots<kWide>, v_slot = (item_base + 1u) % kRingSlots<kWide>;
         // A turn: O_s += P_s V of the stream's tile i, then S_s = Q K^T of its tile i + 1 (which overwrites the P just
         // consumed; the tensor pipe runs them in order), each where the stream has such a tile; i = -1 issues the first S
         // of both streams.  The text of one turn serves both streams and all tiles: with the two streams unrolled (and the
@@ -482,8 +451,8 @@ __device__ __forceinline__ void mma_loop(Aux* aux, uint32_t smem_base, uint32_t 
                     umma_commit_if(s ? issue : 0u, k_empty);
                     tS += 128; q_lo += kQBytes >> 4; s_bar += 8;
                 }
-                k_slot += 2u; if (k_slot >= (uint32_t)kSlots) k_slot -= kSlots;
-                v_slot += 2u; if (v_slot >= (uint32_t)kSlots) v_slot -= kSlots;
+                k_slot += 2u; if (k_slot >= (uint32_t)kRingSlots<kWide>) k_slot -= kRingSlots<kWide>;
+                v_slot += 2u; if (v_slot >= (uint32_t)kRingSlots<kWide>) v_slot -= kRingSlots<kWide>;
                 continue;
             }
 #pragma unroll 1
@@ -493,9 +462,6 @@ __device__ __forceinline__ void mma_loop(Aux* aux, uint32_t smem_base, uint32_t 
                 const bool last_reader = !shared || s == 1;
                 const uint32_t tS = tmem + s * 128;
                 if (do_pv) {
-                    if constexpr (kFp8) {      // K and V arrive apart; where both streams read a tile, the softmax warp of barrier 6 looks
-                        if (!shared) ok = __all_sync(kAll, wait_for_tile<true>(aux, (item_base >> 1) + (uint32_t)(2 * i) + s, 1, abort_flag)) && ok;
-                    }
                     // P of tile i is announced on hardware barrier 4 + s
                     asm volatile("bar.sync %0, %1;" ::"r"(4 + s), "r"(p_threads) : "memory");
                     tc_fence_after();
@@ -522,7 +488,8 @@ __device__ __forceinline__ void mma_loop(Aux* aux, uint32_t smem_base, uint32_t 
                         if (s == 0) asm volatile("bar.sync 6, 64;" ::: "memory");
                     } else if (!(shared && s == 1)) {
                         const uint32_t seq = (item_base >> 1) + (shared ? 0u : (uint32_t)(2 * (i + 1)) + s);
-                        ok = __all_sync(kAll, wait_for_tile<kFp8>(aux, seq, 0, abort_flag)) && ok;
+                        ok = __all_sync(kAll, mbar_wait(smem_u32(&aux->full[seq % kTilesInFlight]), (seq / kTilesInFlight) & 1u,
+                                                        abort_flag)) && ok;
                     }
                     tc_fence_after();
                     const uint32_t issue = ok ? elected : 0u;
@@ -545,8 +512,8 @@ __device__ __forceinline__ void mma_loop(Aux* aux, uint32_t smem_base, uint32_t 
                 // the tiles lie in the ring in the order of the turns that consume them, K and V by turns
                 if (last_reader) {
                     k_slot += 2u;
-                    if (k_slot >= (uint32_t)kSlots) k_slot -= kSlots;
-                    if (i >= 0) { v_slot += 2u; if (v_slot >= (uint32_t)kSlots) v_slot -= kSlots; }
+                    if (k_slot >= (uint32_t)kRingSlots<kWide>) k_slot -= kRingSlots<kWide>;
+                    if (i >= 0) { v_slot += 2u; if (v_slot >= (uint32_t)kRingSlots<kWide>) v_slot -= kRingSlots<kWide>; }
                 }
             }
         }
@@ -596,57 +563,7 @@ __device__ __forceinline__ void store_rows32(const AttnParams& p, float* stage, 
     }
 }
 
-// Q rows for the 8-bit cache: both products are fp16 ones, so a row of bf16 is divided by the power of two that brings its largest
-// element to [2^14, 2^15) - exact but for elements 2^-29 below that - and the row's scores are multiplied by it again, in fp32,
-// along with sm_scale.  Rows beyond M are zeros.
-template <bool kF16>
-__device__ __forceinline__ void load_q_fp8(const AttnParams& p, const Segment& g, AuxFp8* aux, unsigned char* smem, const int s, const int wtid) {
-    const int blk = g.shared ? s : 0, G = p.group;
-    const int r_first = (g.shared ? 0 : 64 * s) + (wtid >> 4), r_count = g.shared ? 16 : 8;      // as in softmax_loop
-    const int c = wtid & 15;
-    unsigned char* dst = smem + blk * kQBytes + (c >> 3) * 16384 + r_first * 128 + (((c & 7) ^ (r_first & 7)) << 4);
-    const unsigned dn = row_node(p, 8), dh = 8u - dn * (unsigned)G;
-    unsigned rr = (unsigned)(blk * 128 + r_first);
-    const unsigned node = row_node(p, rr);
-    unsigned hg = rr - node * (unsigned)G;
-    const __nv_bfloat16* src = p.q + ((long long)(g.node_base + node) * p.num_q_heads + g.h * G + hg) * kHeadDim + c * 8;
-    const long long step = ((long long)dn * p.num_q_heads + dh) * kHeadDim, wrap = (long long)(p.num_q_heads - G) * kHeadDim;
-#pragma unroll 1
-    for (int j0 = 0; j0 < r_count; j0 += 8) {
-        uint4 u[8];
-        const unsigned row0 = rr;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            u[j] = rr < (unsigned)g.M ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
-            rr += 8; src += step; hg += dh;
-            if (hg >= (unsigned)G) { hg -= (unsigned)G; src += wrap; }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float scale = 1.f;
-            if (!kF16) {
-                uint32_t* w = reinterpret_cast<uint32_t*>(&u[j]);
-                uint32_t most = 0u;                    // as bits: the exponent of the largest magnitude
-#pragma unroll
-                for (int i = 0; i < 4; ++i) most = max(most, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-                const int e = max((int)(most >> 23), 27) - 127 - 14;      // -114 .. 114
-                const float inv = __int_as_float((127 - e) << 23);
-                scale = __int_as_float((127 + e) << 23);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    w[i] = pack2_16bit<true>(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
-            }
-            *reinterpret_cast<uint4*>(dst) = u[j];
-            dst += 1024;
-            if (c == 0) aux->row_scale[row0 + 8 * j] = scale;
-        }
-    }
-}
-
-// kF16: q and out are fp16 instead of bf16.
-template <bool kWide, bool kF16, bool kFp8 = false>
+template <bool kWide, bool kF16>
 __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsigned char* smem, uint32_t tmem,
                                              const int s /*stream*/) {
     const int wtid = threadIdx.x - 128 - s * 128;          // 0..127 inside the warpgroup
@@ -654,8 +571,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
     volatile int* abort_flag = &aux->abort_flag;
     const uint32_t lane_sel = (uint32_t)(((threadIdx.x >> 5) & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_sel + s * 128;
-    constexpr bool kP16 = kF16 || kFp8;                      // the weights are fp16
-    float scale2 = p.sm_scale * 1.4426950408889634f;         // > 0 (checked on the host)
+    const float scale2 = p.sm_scale * 1.4426950408889634f;   // > 0 (checked on the host)
     const int G = p.group;
     uint32_t it = 0, seg_no = 0, od_phase = 0;   // od_phase: segments of this stream that issued a product
     uint32_t tile_base = 0;                      // key tiles of the CTA's earlier segments (the ring counts them through)
@@ -671,8 +587,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
         if (s == 0 && wtid < g.n) parent_i = p.tree_parent[g.node_base + wtid];
         if (seg_no > 0) named_barrier(1, 256);   // the other warpgroup may still be reading its staging area in the Q block
         if (leader) const_cast<volatile int&>(aux->seg_reached) = (int)seg_no;
-        if constexpr (kFp8) load_q_fp8<kF16>(p, g, static_cast<AuxFp8*>(aux), smem, s, wtid);
-        else {
+        {
             // shared: this warpgroup loads its own 128-row block; split: rows [64 s, 64 s + 64) of block 0
             const int blk = g.shared ? s : 0;
             const int r_first = (g.shared ? 0 : 64 * s) + (wtid >> 4);
@@ -723,7 +638,6 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
 
         const int rr = (g.shared ? s * 128 : 0) + row_local;       // packed row of this thread
         const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
-        if constexpr (kFp8) scale2 = p.sm_scale * 1.4426950408889634f * static_cast<AuxFp8*>(aux)->row_scale[rr];
         const int n_it = g.iters(s);
         const int live = g.template live_warps<kWide>();
         const bool idle = (wtid >> 5) >= live;       // no row of the unit in this warp: straight to the segment's end
@@ -765,9 +679,8 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
                 // tile's arrival barrier covers V as well as K, so the rows have landed; the stores are ordered
                 // before the product by the proxy fence here and the hand-off of P below.  Both warpgroups of a
                 // 256-row unit do it (zeros over zeros); the slot is not released before both products are done.
-                // (The 8-bit cache's converting warps zero them themselves.)
                 const int kv_valid = g.L + g.n - t * kTileKeys;            // >= 1 valid keys in this tile
-                if (!kFp8 && kv_valid < kTileKeys) {
+                if (kv_valid < kTileKeys) {
                     const int kv_end = min(kTileKeys, ((kv_valid + p.page_size - 1) >> p.page_shift) << p.page_shift);
                     const uint32_t seq = tile_base + (uint32_t)(g.shared ? i : 2 * i + s);
                     unsigned char* vslot = smem + kRingOff<kWide> + ((2u * seq + 1u) % kRingSlots<kWide>) * kSlotBytes;
@@ -787,7 +700,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
             // is redone the long way.
             bool done = false, force = false;
             if (i > 0 && !__any_sync(0xffffffffu, m == -INFINITY)) {
-                const uint64_t scale2_x2 = pack_f32x2(scale2, scale2), neg_m_x2 = pack_f32x2(kWeightShift<kFp8> - m, kWeightShift<kFp8> - m);
+                const uint64_t scale2_x2 = pack_f32x2(scale2, scale2), neg_m_x2 = pack_f32x2(-m, -m);
                 uint64_t ex_a = 0ull, ex_b = 0ull, rs_a = 0ull, rs_b = 0ull;
                 uint32_t pk[64];
                 uint32_t buf_a[32], buf_b[32];
@@ -805,11 +718,11 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
                                                       scale2_x2, neg_m_x2);
                         unpack_f32x2(xx, x0, x1);
                         const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                        const uint32_t u = pack2_16bit<kP16>(p0, p1);
+                        const uint32_t u = pack2_16bit<kF16>(p0, p1);
                         pk[c4 * 16 + j] = u;
                         const uint64_t pe = pack_f32x2(p0, p1);
                         uint64_t pr;      // the two weights as the tensor core will read them
-                        if (kP16) {
+                        if (kF16) {
                             const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&u));
                             pr = pack_f32x2(r.x, r.y);
                         } else {
@@ -824,7 +737,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
                 unpack_f32x2(add_f32x2(ex_a, ex_b), b0, b1);
                 // no weight can exceed the tile's sum: a sum of at most 2^8 means that no score is more than the lazy
                 // threshold above m (a larger sum sends the tile the long way, which then moves m up)
-                force = (b0 + b1) > (kFp8 ? 32768.f : 256.f);
+                force = (b0 + b1) > 256.f;
                 if (!__any_sync(0xffffffffu, force)) {
                     tmem_st32(tS, reinterpret_cast<uint32_t(&)[32]>(pk[0]));
                     tmem_st32(tS + 32, reinterpret_cast<uint32_t(&)[32]>(pk[32]));
@@ -876,7 +789,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
                     }
                     m = m_new;
                 }
-                const float neg_m = (m == -INFINITY) ? 0.f : kWeightShift<kFp8> - m;
+                const float neg_m = (m == -INFINITY) ? 0.f : -m;
                 const uint64_t scale2_x2 = pack_f32x2(scale2, scale2), neg_m_x2 = pack_f32x2(neg_m, neg_m);
                 // two packed accumulators each for the exact sum (LSE) and for the sum of the rounded weights: the
                 // normaliser takes the very numbers P V multiplies by, so that out = sum(p v) / sum(p) stays a true
@@ -894,11 +807,11 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
                         const uint64_t xx = fma_f32x2(pack_f32x2(__uint_as_float(sv[2 * j]), __uint_as_float(sv[2 * j + 1])), scale2_x2, neg_m_x2);
                         unpack_f32x2(xx, x0, x1);
                         const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                        const uint32_t u = pack2_16bit<kP16>(p0, p1);
+                        const uint32_t u = pack2_16bit<kF16>(p0, p1);
                         pk[j] = u;
                         const uint64_t pe = pack_f32x2(p0, p1);
                         uint64_t pr;      // the two weights as the tensor core will read them
-                        if (kP16) {
+                        if (kF16) {
                             const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&u));
                             pr = pack_f32x2(r.x, r.y);
                         } else {
@@ -919,8 +832,6 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
             }
             tmem_wait_st();
             tc_fence_before();
-            // (8-bit cache, both streams on one tile: the V tile has been turned into fp16; stream 1's product follows stream 0's)
-            if (kFp8 && kWide && g.shared && s == 0 && wtid < 32) wait_for_tile<true>(aux, tile_base + (uint32_t)i, 1, abort_flag);
             // Hand-off of P: hardware barrier 4 + s, the live warps of this warpgroup + the MMA warp.  Executed once per
             // key tile of this stream - n_it times per segment, the count of the MMA warp's bar.sync on it - on every
             // path: nothing above leaves the loop body early.  S of this tile has been announced, on every path too, so
@@ -933,7 +844,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
             // that gives up raises the abort flag; the arrival happens all the same.
             if (g.shared && s == 0 && wtid < 32 && i + 1 < n_it) {
                 const uint32_t seq = tile_base + (uint32_t)(i + 1);
-                wait_for_tile<kFp8>(aux, seq, 0, abort_flag);
+                mbar_wait(smem_u32(&aux->full[seq % kTilesInFlight]), (seq / kTilesInFlight) & 1u, abort_flag);
                 // hardware barrier 6, 64 threads (this warp + the MMA warp): once per tile but the segment's last,
                 // T - 1 times, matching the MMA warp's bar.sync 6 before S of tiles 1 .. T - 1; unconditional
                 asm volatile("bar.arrive 6, 64;" ::: "memory");
@@ -981,7 +892,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
         int c_first = 0, c_count = 4;
         if (g.shared) {
             wa = l > 0.f ? 1.f / l : 0.f;
-            lse = lx > 0.f ? (m - kWeightShift<kFp8> + __log2f(lx)) * 0.6931471805599453f : -INFINITY;
+            lse = lx > 0.f ? (m + __log2f(lx)) * 0.6931471805599453f : -INFINITY;
         } else {
             // (a stream without a tile has m = -inf and nothing in its sums)
             use_b = g.iters(1) > 0;
@@ -1007,7 +918,7 @@ __device__ __forceinline__ void softmax_loop(const AttnParams& p, Aux* aux, unsi
             const float lt = a0 * l0 + a1 * l1, xt = a0 * x0 + a1 * x1;
             const float inv = lt > 0.f ? 1.f / lt : 0.f;
             wa = a0 * inv; wb = a1 * inv;
-            lse = xt > 0.f ? (mm - kWeightShift<kFp8> + __log2f(xt)) * 0.6931471805599453f : -INFINITY;
+            lse = xt > 0.f ? (mm + __log2f(xt)) * 0.6931471805599453f : -INFINITY;
             tOa = tmem + lane_sel + 256;
             write_lse = s == 0;
             c_first = 2 * s; c_count = 2;
