@@ -20,13 +20,18 @@
 //   warps 4-11    softmax, two streams
 //   warps 12-15   turn V into fp16, two slots of 32 KB
 //
-// Which operand has the lanes.  Units of more than 64 rows: the rows of Q (S and P as in verify_attn_umma.cuh, P in tensor memory).  Units of
-// up to 64 rows ("keys on lanes"): the products are turned round,
-//   S^T = K Q^T   [128 keys x pieces * rows], the pieces' columns added up in registers,
-//   O^T += V^T P  [128 channels x rows],      P [keys x rows] through shared memory,
-// so that a unit of 32 rows does not pay for 128 of them: the products take an eighth and a quarter of the multipliers (and of the power,
-// which is what sets the clock here), a softmax thread has one key and all rows, every lane is in use, and sums over keys are
-// kept per thread until the segment's end.
+// Units of more than 128 rows ("shared"): two streams of 128 rows on the same tiles, each with its S, P and O in tensor memory, as in
+// verify_attn_umma.cuh.
+// Other units ("joint"): both softmax warpgroups work on each tile, one O, and three S, so that Q K^T runs up to three tiles ahead and no
+// softmax waits for the products of the tile before.  (With two streams that took the tiles by turns, each waiting for its own
+// P V and Q K^T, a 128-row tile took 2100 clocks: %J1%.)
+//   65 to 128 rows: rows on the lanes, each warpgroup weighs half of a tile's keys; the two share the rows' references.
+//   up to 64 rows:  keys on the lanes.  The products are turned round,
+//       S^T = K Q^T   [128 keys x pieces * rows], the pieces' columns added up in registers,
+//       O^T += V^T P  [128 channels x rows],      P [keys x rows] through shared memory,
+//     so that a unit of 32 rows does not pay for 128 of them: the products take an eighth and a quarter of the multipliers (and of the
+//     power, which is what sets the clock here), a softmax thread has one key and half of the rows, every lane is in use, and sums
+//     over keys are kept per thread until the segment's end.
 #pragma once
 
 #include "fp8_block.cuh"
@@ -39,7 +44,7 @@ constexpr int kFp8Threads = 512;
 constexpr int kPieceBytes = 128 * kHeadDim;          // 16 KB: one piece of 128 rows of Q; also a raw K or V tile
 constexpr int kFp8VSlots = 2;                        // fp16 V tiles, 32 KB each
 constexpr int kNotes = 8;
-constexpr int kRowsOfPartial = kRows;                // (`kRows` below is also a parameter's name)
+constexpr int kPartialRows = kRows;                  // (`kRows` below is also a constant of a template)
 constexpr int kKeysRows = 64;                        // most rows of a unit with its keys on the lanes
 constexpr int kPBytes = kTileKeys * 128;             // its P: 128 bytes (64 rows) per key, one per stream
 // Shared memory: Q (its pieces; keys on lanes: fewer rows, then the two P), the fp16 V tiles, the ring of raw tiles, scratch.
@@ -50,35 +55,42 @@ template <bool kWide, bool kF16> constexpr int kVOff = larger((kWide ? 2 : 1) * 
 template <bool kWide, bool kF16> constexpr int kRawOff = kVOff<kWide, kF16> + kFp8VSlots * kSlotBytes;
 template <bool kWide, bool kF16> constexpr int kRawTiles = (kAuxOff - kRawOff<kWide, kF16>) / (2 * kPieceBytes);
 static_assert(kRawTiles<false, false> == 3 && kRawTiles<false, true> == 3 && kRawTiles<true, false> == 3 && kRawTiles<true, true> == 2, "layout");
-// Keys on lanes: the rows' numbers, one set per stream.
+// Joint units' numbers of their rows.
 struct KeysScratch {
-    float scale[2][kKeysRows], bias[2][kKeysRows];   // a weight is exp2(score * scale + bias)
-    float m[2][kKeysRows], alpha[2][32];
-    unsigned most[2][32];                            // largest score of the tile, as an ordered integer
-    float sum[2][4][kKeysRows];                      // of the weights, by warp
-    float w[2][kKeysRows];                           // what the streams' O are multiplied by
+    float scale[kKeysRows], bias[kKeysRows];         // a weight is exp2(score * scale + bias)
+    float m[kKeysRows], alpha[kKeysRows];
+    unsigned most[4][kKeysRows];                     // largest score of the tile by warp, as an ordered integer
+    float sum[4][kKeysRows];                         // of the weights, by warp
+    float w[kKeysRows];                              // what O is multiplied by
 };
+struct RowsScratch {
+    float most[2][128], sum[2][128];                 // by warpgroup
+};
+static_assert(sizeof(RowsScratch) <= sizeof(KeysScratch), "the larger one is counted");
 template <bool kWide, bool kF16> constexpr int kScratchOff = kWide ? kPOff<kF16> + 2 * kPBytes : kRawOff<kWide, kF16> + kRawTiles<kWide, kF16> * 2 * kPieceBytes;
 static_assert(kScratchOff<false, false> + sizeof(KeysScratch) <= kAuxOff && kScratchOff<false, true> + sizeof(KeysScratch) <= kAuxOff, "layout");
 static_assert(kScratchOff<true, false> + sizeof(KeysScratch) <= kVOff<true, false> && kScratchOff<true, true> + sizeof(KeysScratch) <= kVOff<true, true>, "layout");
-// Tensor memory: S0 S1 O0 O1 of 128 columns; keys on lanes: two S of up to 192, two O of 64.
-constexpr uint32_t kKeysS = 192, kKeysO = 384;
+// Tensor memory: shared S0 S1 O0 O1 of 128 columns; joint three S of 128 columns (two of 192: fp16, 64 rows, keys on lanes) and O.
+constexpr uint32_t kJointO = 384;
+__device__ __forceinline__ uint32_t joint_buffers(uint32_t columns) { return columns > 128u ? 2u : 3u; }
+__device__ __forceinline__ uint32_t joint_s(uint32_t buffer, uint32_t columns) { return buffer * (columns > 128u ? 192u : 128u); }
 
 // What is known of a tile besides its bytes.  A place is written again eight tiles later: the producer is at most kRawTiles ahead of
-// the products, and those one tile per stream ahead of the softmax warps, the last to look at it.
+// Q K^T, and that at most three tiles ahead of the softmax warps, the last to look at it.
 struct TileNote {
     float kscale[kTileKeys / 16];                // 2^e of K, for each 16 keys
     int valid;                                   // keys of the sequence in it; -1: no more tiles
     int8_t vexp[kTileKeys / 16];                 // e of V
 };
 struct AuxFp8 : Aux {
-    uint64_t raw_full[8], raw_empty[8];          // K and V of each raw tile
+    uint64_t raw_full[6], raw_empty[6];          // K and V of each raw tile
     uint64_t v_full[kFp8VSlots], v_empty[kFp8VSlots];
+    uint64_t joint_s_full[3], joint_o_done;
     TileNote note[kNotes];
     float row_scale[kRows];                      // what the rows of Q were divided by
 };
 static_assert(sizeof(AuxFp8) <= kAuxBytes, "aux area too small");
-static_assert(kNotes >= 4 + 2, "a note outlives its tile's place in the ring");
+static_assert(kNotes > 3 + 3, "a note outlives its tile's place in the ring");
 
 // Rows that a unit with its keys on the lanes is padded to; 0: its rows are on the lanes.
 __device__ __forceinline__ int keys_rows(int M) { return M <= 32 ? 32 : M <= kKeysRows ? 64 : 0; }
@@ -237,8 +249,8 @@ __device__ __forceinline__ void convert_loop(const AttnParams& p, AuxFp8* aux, u
 }
 
 // ------------------------------------------------------------------------------------------ MMA issuer
-// mma_loop's turns and hand-offs.  K arrives in the raw ring, V apart from it as an fp16 tile; both streams on one tile (256 rows): the
-// softmax warp that looks at the next K tile for this warp also makes sure of V before it announces P.
+// K arrives in the raw ring, V apart from it as an fp16 tile.  In shared units the softmax warp that looks at the next K tile for this warp
+// also makes sure of V before it announces P.
 template <bool kWide, bool kF16>
 __device__ __forceinline__ void mma_loop_fp8(AuxFp8* aux, uint32_t smem_base, uint32_t tmem) {
     constexpr unsigned kAll = 0xffffffffu;
@@ -254,7 +266,7 @@ __device__ __forceinline__ void mma_loop_fp8(AuxFp8* aux, uint32_t smem_base, ui
     const uint32_t q_hi = (uint32_t)(q_desc0 >> 32), k_hi = (uint32_t)(k_desc0 >> 32), v_hi = (uint32_t)(v_desc0 >> 32);
     const uint32_t raw_full = smem_u32(&aux->raw_full[0]), raw_empty = smem_u32(&aux->raw_empty[0]);
     const uint32_t v_full = smem_u32(&aux->v_full[0]), v_empty = smem_u32(&aux->v_empty[0]);
-    const uint32_t s_full = smem_u32(&aux->s_full[0]), o_done = smem_u32(&aux->o_done[0]);
+    const uint32_t s_full = smem_u32(&aux->s_full[0]), o_done = smem_u32(&aux->o_done[0]), joint_s_full = smem_u32(&aux->joint_s_full[0]);
     uint32_t seg_no = 0, k_place = 0, k_parity = 0, v_seq = 0;
 
     auto qk = [&](uint32_t issue, uint32_t tS, uint32_t q_lo) {
@@ -272,24 +284,29 @@ __device__ __forceinline__ void mma_loop_fp8(AuxFp8* aux, uint32_t smem_base, ui
         for (int ks = 0; ks < 8; ++ks)
             umma_ts_lh_if(issue, tS + 256, tS + ks * 8, v_lo + (uint32_t)(ks * 4096 >> 4), v_hi, idesc_pv, ks ? 1u : accumulate);
     };
-    // keys on lanes, `rows` padded rows
+    // joint units; `keys`: keys on lanes, the padded rows
     const uint64_t p_desc0 = umma_smem_desc_sw128(smem_base + kPOff<kF16>, 1024, 1024);
-    auto qk_keys = [&](uint32_t issue, uint32_t s, uint32_t rows) {
+    auto qk_joint = [&](uint32_t issue, uint32_t tS, uint32_t keys) {
+        if (!keys) { qk(issue, tS, (uint32_t)q_desc0); return; }
         const uint32_t k_lo = (uint32_t)k_desc0 + k_place * (uint32_t)(2 * kPieceBytes >> 4);
-        const uint32_t idesc = umma_idesc_e4m3(128, 0) | (kPieces<kF16> * rows >> 3) << 17;
+        const uint32_t idesc = umma_idesc_e4m3(128, 0) | (kPieces<kF16> * keys >> 3) << 17;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
-            umma_f8_ss_lh_if(issue, tmem + s * kKeysS, k_lo + (uint32_t)(ks * 32 >> 4), k_hi, (uint32_t)q_desc0 + (uint32_t)(ks * 32 >> 4), q_hi, idesc,
-                             ks ? 1u : 0u);
+            umma_f8_ss_lh_if(issue, tS, k_lo + (uint32_t)(ks * 32 >> 4), k_hi, (uint32_t)q_desc0 + (uint32_t)(ks * 32 >> 4), q_hi, idesc, ks ? 1u : 0u);
     };
-    auto pv_keys = [&](uint32_t issue, uint32_t s, uint32_t rows, uint32_t accumulate) {
-        const uint32_t v_lo = (uint32_t)v_desc0 + (v_seq % kFp8VSlots) * (uint32_t)(kSlotBytes >> 4);
-        const uint32_t p_lo = (uint32_t)p_desc0 + s * (uint32_t)(kPBytes >> 4), p_hi = (uint32_t)(p_desc0 >> 32);
-        const uint32_t idesc = umma_idesc_16bit(128, 0, 1, 1, true) | rows >> 3 << 17;
+    auto pv_joint = [&](uint32_t issue, uint32_t tP, uint32_t i, uint32_t keys) {
+        const uint32_t v_lo = (uint32_t)v_desc0 + (v_seq % kFp8VSlots) * (uint32_t)(kSlotBytes >> 4), acc0 = i > 0 ? 1u : 0u;
+        if (!keys) {
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+                umma_ts_lh_if(issue, tmem + kJointO, tP + ks * 8, v_lo + (uint32_t)(ks * 4096 >> 4), v_hi, idesc_pv, ks ? 1u : acc0);
+            return;
+        }
+        const uint32_t p_lo = (uint32_t)p_desc0 + (i & 1u) * (uint32_t)(kPBytes >> 4), p_hi = (uint32_t)(p_desc0 >> 32);
+        const uint32_t idesc = umma_idesc_16bit(128, 0, 1, 1, true) | keys >> 3 << 17;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
-            umma_ss_lh_if(issue, tmem + kKeysO + s * 64, v_lo + (uint32_t)(ks * 4096 >> 4), v_hi, p_lo + (uint32_t)(ks * 2048 >> 4), p_hi, idesc,
-                          ks ? 1u : accumulate);
+            umma_ss_lh_if(issue, tmem + kJointO, v_lo + (uint32_t)(ks * 4096 >> 4), v_hi, p_lo + (uint32_t)(ks * 2048 >> 4), p_hi, idesc, ks ? 1u : acc0);
     };
     auto next_k = [&] { if (++k_place == kPlaces) { k_place = 0; k_parity ^= 1u; } };
 
@@ -299,90 +316,83 @@ __device__ __forceinline__ void mma_loop_fp8(AuxFp8* aux, uint32_t smem_base, ui
         const int tile0 = __reduce_max_sync(kAll, g.tile0), tile1 = __reduce_max_sync(kAll, g.tile1);
         if (tile1 == 0) break;
         const bool shared = kWide && __reduce_max_sync(kAll, g.shared ? 1 : 0) != 0;
-        const int p_threads = kWide ? 160 : 32 + 32 * __reduce_max_sync(kAll, live_warps_fp8(g.M));
-        const uint32_t keys = (uint32_t)__reduce_max_sync(kAll, keys_rows(g.M));      // keys on lanes: the padded rows
         bool ok = __all_sync(kAll, mbar_wait(smem_u32(&aux->q_full), seg_no & 1u, abort_flag));
         const int T = tile1 - tile0;
-        const int n_it[2] = {shared ? T : (T + 1) >> 1, shared ? T : T >> 1};
-#pragma unroll 1
-        for (int i = -1; i < n_it[0]; ++i) {
-            if (kWide && shared && ok && i >= 0 && i + 1 < T) {      // the middle of a 256-row unit: a turn without conditions
-                const uint32_t acc0 = i > 0 ? 1u : 0u;
-                uint32_t q_lo = (uint32_t)q_desc0, tS = tmem, s_bar = s_full;
-                const uint32_t v_bar = v_empty + (v_seq % kFp8VSlots) * 8u, k_bar = raw_empty + k_place * 16u;
-#pragma unroll 1
-                for (uint32_t s = 0; s < 2; ++s) {
-                    asm volatile("bar.sync %0, 160;" ::"r"(4 + s) : "memory");
-                    tc_fence_after();
-                    pv(elected, tS, acc0);
-                    umma_commit_if(s ? elected : 0u, v_bar);
-                    if (s == 0) asm volatile("bar.sync 6, 64;" ::: "memory");
-                    qk(elected, tS, q_lo);
-                    umma_commit_if(elected, s_bar);
-                    umma_commit_if(s ? elected : 0u, k_bar);
-                    tS += 128; q_lo += (uint32_t)(kPieces<kF16> * kPieceBytes >> 4); s_bar += 8;
-                }
+        ++seg_no;
+        if (!shared) {
+            const uint32_t keys = (uint32_t)__reduce_max_sync(kAll, keys_rows(g.M)), columns = keys ? kPieces<kF16> * keys : 128u;
+            const int p_threads = 32 + 64 * __reduce_max_sync(kAll, live_warps_fp8(g.M)), ahead = (int)joint_buffers(columns);
+            uint32_t b = 0, p_bar = 0;              // S buffer of the tile; hardware barrier of its P, 9 + p_bar
+            // S = Q K^T of the segment's next tile, announced on every path (mma_loop says why)
+            auto next_s = [&] {
+                ok = __all_sync(kAll, mbar_wait(raw_full + k_place * 16u, k_parity, abort_flag)) && ok;
+                tc_fence_after();
+                const uint32_t issue = ok ? elected : 0u;
+                qk_joint(issue, tmem + joint_s(b, columns), keys);
+                umma_commit_if(issue, joint_s_full + b * 8u);
+                if (!ok && elected) mbar_arrive(joint_s_full + b * 8u);
+                umma_commit_if(issue, raw_empty + k_place * 16u);
                 next_k();
+            };
+            for (int i = 0; i < ahead && i < T; ++i) { b = (uint32_t)i; next_s(); }
+            b = 0;
+#pragma unroll 1
+            for (int i = 0; i < T; ++i) {
+                // V is looked at while P is being made; then P is announced on hardware barrier 9, 10 or 11, each every third tile: a warp
+                // that arrives for tile i + 3 has seen its S, which is issued after this warp's bar.sync for tile i (so one
+                // generation never sees two tiles' arrivals)
+                ok = __all_sync(kAll, mbar_wait(v_full + (v_seq % kFp8VSlots) * 8u, (v_seq / kFp8VSlots) & 1u, abort_flag)) && ok;
+                asm volatile("bar.sync %0, %1;" ::"r"(9 + p_bar), "r"(p_threads) : "memory");
+                tc_fence_after();
+                const uint32_t issue = ok ? elected : 0u;
+                pv_joint(issue, tmem + joint_s(b, columns), (uint32_t)i, keys);
+                umma_commit_if(issue, v_empty + (v_seq % kFp8VSlots) * 8u);
+                if (i == T - 1) {
+                    umma_commit_if(issue, smem_u32(&aux->joint_o_done));
+                    if (!ok && elected) mbar_arrive(smem_u32(&aux->joint_o_done));
+                }
                 ++v_seq;
-                continue;
+                // the product that reads this tile's P has been issued: its S buffer takes the tile `ahead` tiles on
+                if (i + ahead < T) next_s();
+                if (++b == (uint32_t)ahead) b = 0;
+                if (++p_bar == 3u) p_bar = 0;
             }
-            if (!shared && ok && i >= 0 && i + 1 < n_it[1]) {        // of another unit: both streams have both products
+            continue;
+        }
+        if constexpr (kWide) {
+            // two streams of 128 rows on the same tiles: mma_loop's turns
+#pragma unroll 1
+            for (int i = -1; i < T; ++i) {
+                const bool do_pv = i >= 0, do_qk = i + 1 < T;
+                const uint32_t v_bar = v_empty + (v_seq % kFp8VSlots) * 8u, k_bar = raw_empty + k_place * 16u;
+                uint32_t q_lo = (uint32_t)q_desc0, tS = tmem;
+                if (i < 0) ok = __all_sync(kAll, mbar_wait(raw_full + k_place * 16u, k_parity, abort_flag)) && ok;
+                tc_fence_after();
+                const uint32_t issue = ok ? elected : 0u;
 #pragma unroll 1
                 for (uint32_t s = 0; s < 2; ++s) {
-                    const uint32_t tS = tmem + s * 128;
-                    asm volatile("bar.sync %0, %1;" ::"r"(4 + s), "r"(p_threads) : "memory");
-                    tc_fence_after();
-                    if (keys) pv_keys(elected, s, keys, i > 0 ? 1u : 0u);
-                    else pv(elected, tS, i > 0 ? 1u : 0u);
-                    umma_commit_if(elected, v_empty + (v_seq % kFp8VSlots) * 8u);
-                    ++v_seq;
-                    if (keys) qk_keys(elected, s, keys);
-                    else qk(elected, tS, (uint32_t)q_desc0);
-                    umma_commit_if(elected, s_full + s * 8u);
-                    umma_commit_if(elected, raw_empty + k_place * 16u);
-                    next_k();
-                }
-                continue;
-            }
-#pragma unroll 1
-            for (uint32_t s = 0; s < 2; ++s) {
-                const int n_s = s ? n_it[1] : n_it[0];
-                const bool do_pv = i >= 0 && i < n_s, do_qk = i + 1 < n_s;
-                const bool last_reader = !shared || s == 1;
-                const uint32_t tS = tmem + s * 128;
-                if (do_pv) {
-                    // P of tile i is announced on hardware barrier 4 + s (and with it V of the tile and, but for 256-row units, the stream's
-                    // next K)
-                    asm volatile("bar.sync %0, %1;" ::"r"(4 + s), "r"(p_threads) : "memory");
-                    tc_fence_after();
-                    const uint32_t issue = ok ? elected : 0u;
-                    if (keys) pv_keys(issue, s, keys, i > 0 ? 1u : 0u);
-                    else pv(issue, tS, i > 0 ? 1u : 0u);
-                    // only the segment end waits for it; made on every path, like the announcement of S below
-                    umma_commit_if(i == n_s - 1 ? issue : 0u, o_done + s * 8u);
-                    if (!ok && i == n_s - 1 && elected) mbar_arrive(o_done + s * 8u);
-                    umma_commit_if(last_reader ? issue : 0u, v_empty + (v_seq % kFp8VSlots) * 8u);
-                    if (last_reader) ++v_seq;
-                }
-                if (do_qk) {
-                    if (i >= 0) {
-                        if (shared && s == 0) asm volatile("bar.sync 6, 64;" ::: "memory");
-                    } else if (!(shared && s == 1)) {
-                        ok = __all_sync(kAll, mbar_wait(raw_full + k_place * 16u, k_parity, abort_flag)) && ok;
+                    if (do_pv) {
+                        // P of the tile (and that V has been turned into fp16) is announced on hardware barrier 4 + s
+                        asm volatile("bar.sync %0, 160;" ::"r"(4 + s) : "memory");
+                        tc_fence_after();
+                        pv(issue, tS, i > 0 ? 1u : 0u);
+                        umma_commit_if(s ? issue : 0u, v_bar);
+                        umma_commit_if(do_qk ? 0u : issue, o_done + s * 8u);
+                        if (!ok && !do_qk && elected) mbar_arrive(o_done + s * 8u);
                     }
-                    tc_fence_after();
-                    const uint32_t issue = ok ? elected : 0u;
-                    if (keys) qk_keys(issue, s, keys);
-                    else qk(issue, tS, (uint32_t)q_desc0 + ((shared && s) ? (uint32_t)(kPieces<kF16> * kPieceBytes >> 4) : 0u));
-                    // S is announced on every path (mma_loop says why)
-                    umma_commit_if(issue, s_full + s * 8u);
-                    if (!ok && elected) mbar_arrive(s_full + s * 8u);
-                    umma_commit_if(last_reader ? issue : 0u, raw_empty + k_place * 16u);
-                    if (last_reader) next_k();
+                    if (do_qk) {
+                        if (do_pv && s == 0) asm volatile("bar.sync 6, 64;" ::: "memory");      // the next K tile has landed
+                        qk(issue, tS, q_lo);
+                        umma_commit_if(issue, s_full + s * 8u);
+                        if (!ok && elected) mbar_arrive(s_full + s * 8u);
+                        umma_commit_if(s ? issue : 0u, k_bar);
+                    }
+                    tS += 128; q_lo += (uint32_t)(kPieces<kF16> * kPieceBytes >> 4);
                 }
+                if (do_pv) ++v_seq;
+                if (do_qk) next_k();
             }
         }
-        ++seg_no;
     }
 }
 
@@ -450,7 +460,488 @@ __device__ __forceinline__ void load_q_fp8(const AttnParams& p, const Segment& g
 // key has all the weight, and two conversions and an addition per pair of keys less (70B with 32 nodes 647 -> 592 us).
 constexpr float kWeightShift = 7.f;
 constexpr float kWeightLimit = 32768.f;          // 2^(8 + 7)
-// Rows on lanes: the weights of a tile against the running maximum m, 32 columns of S at a time.  False, with nothing stored, if some
+// log-sum-exp of a row from its reference and its sum of shifted weights (a NaN sum stays one)
+__device__ __forceinline__ float lse_of_sum(float m, float sum) {
+    return sum > 0.f ? (m - kWeightShift + __log2f(sum)) * 0.6931471805599453f : sum == 0.f ? -INFINITY : sum;
+}
+__device__ __forceinline__ unsigned ordered(float x) {        // sorts like x; a NaN is below everything
+    const unsigned u = __float_as_uint(x);
+    return x != x ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(unsigned u) { return u == 0u ? -INFINITY : __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+__device__ __forceinline__ float min_or_nan(float x, float y) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+// Meets `count` threads on hardware barrier `id`; true for all if it is for one.
+__device__ __forceinline__ bool any_of(int id, int count, bool mine) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+                 : "=r"(r) : "r"(id), "r"(count), "r"(mine ? 1u : 0u) : "memory");
+    return r != 0;
+}
+
+// What a segment's threads know of it, in either kind of joint unit.
+struct JointSegment {
+    const Segment& g;
+    uint32_t tile_base, seg_no;      // the CTA's key tiles and segments so far
+    bool leader;
+};
+// The product O += P V of key tile `seq` has completed.  (Its barrier's next phase is that of tile seq + 2, whose P has not been handed
+// over.)
+__device__ __forceinline__ void wait_for_product(AuxFp8* aux, uint32_t seq) {
+    mbar_wait(smem_u32(&aux->v_empty[seq % kFp8VSlots]), (seq / kFp8VSlots) & 1u, &aux->abort_flag);
+    __syncwarp();
+    tc_fence_after();
+}
+// S of the segment's tile i, in buffer `b`; `phases`: one bit per buffer, the phase of its barrier that comes next.
+__device__ __forceinline__ void wait_for_scores(AuxFp8* aux, uint32_t b, uint32_t& phases) {
+    mbar_wait_certain(smem_u32(&aux->joint_s_full[b]), (phases >> b) & 1u, &aux->abort_flag);
+    phases ^= 1u << b;
+    tc_fence_after();
+}
+
+// ------------------------------------------------------------------------------------------ joint units, rows on lanes
+// Warpgroup s has the tile's keys [64 s, 64 s + 64); thread = row, in both.
+template <bool kWide, bool kF16>
+__device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s, const JointSegment& js,
+                                             uint32_t& phases, const uint32_t done_phase) {
+    const Segment& g = js.g;
+    const int wtid = threadIdx.x - 128 - s * 128;
+    const uint32_t lane_sel = (uint32_t)(((threadIdx.x >> 5) & 3) * 32) << 16;
+    RowsScratch* k = reinterpret_cast<RowsScratch*>(smem + kScratchOff<kWide, kF16>);
+    const int T = g.tile1 - g.tile0, rr = wtid, G = p.group;
+    const int live = live_warps_fp8(g.M), both = 64 * live;      // threads of the two warpgroups that hold rows
+    const bool idle = (wtid >> 5) >= live;
+    const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
+    const float scale2 = p.sm_scale * 1.4426950408889634f * aux->row_scale[rr];
+    float m = -INFINITY, l = 0.f;          // the row's reference, alike in both warpgroups; the sum over this one's keys
+    uint32_t b = 0, p_bar = 0;
+    for (int i = 0; i < (idle ? 0 : T); ++i) {
+        const int t = g.tile0 + i;
+        const uint32_t seq = js.tile_base + (uint32_t)i;
+        wait_for_scores(aux, b, phases);
+        const uint32_t tS = tmem + lane_sel + joint_s(b, 128u), tMine = tS + 64 * s;
+        const float* kscale = aux->note[seq % kNotes].kscale + 4 * s;
+        if ((t + 1) * kTileKeys > g.L) {
+            // The tile reaches drafted positions (or the end of the sequence): at most two tiles per unit.
+            // Visibility of this warpgroup's 64 keys for this row: prefix keys all, drafted key j iff ancestor-or-self.  The mask is
+            // applied to S in tensor memory before the common path reads it.
+            const int j0 = t * kTileKeys + 64 * s - g.L;
+            const unsigned long long sees = j0 >= 64 ? 0ull : j0 >= 0 ? anc_row >> j0 : j0 <= -64 ? ~0ull : (~0ull >> (64 + j0)) | (anc_row << -j0);
+#pragma unroll 1
+            for (int c = 0; c < 2; ++c) {
+                const uint32_t bits = (uint32_t)(sees >> (32 * c));
+                uint32_t r[32];
+                tmem_ld32(tMine + c * 32, r);
+                tmem_wait_ld();
+                tmem_loaded(r);
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (!((bits >> j) & 1u)) r[j] = 0xff800000u;   // -inf
+                tmem_st32(tMine + c * 32, r);
+            }
+            tmem_wait_st();
+        }
+        uint32_t pk[32];
+        float sum;
+        // up to three times: the references hold; some score was above its by more than the threshold; the first tile
+        for (int tries = i == 0 ? 0 : 1;; ++tries) {
+            if (tries != 1) {
+                // the references move up to the tile's largest scores; the two warpgroups exchange theirs
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t r[32];
+                    tmem_ld32(tMine + c * 32, r);
+                    tmem_wait_ld();
+                    tmem_loaded(r);
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        float a = __uint_as_float(r[16 * hf]);
+#pragma unroll
+                        for (int j = 1; j < 16; ++j) a = fmaxf(a, __uint_as_float(r[16 * hf + j]));
+                        mx = fmaxf(mx, a * (kscale[2 * c + hf] * scale2));
+                    }
+                }
+                k->most[s][wtid] = mx;
+                named_barrier(8, both);
+                const float m_new = fmaxf(m, fmaxf(mx, k->most[s ^ 1][wtid]));
+                if (i > 0 && __any_sync(0xffffffffu, m_new > m)) {
+                    const float alpha = m_new > m ? fast_exp2(m - m_new) : 1.f;
+                    l *= alpha;
+                    wait_for_product(aux, seq - 1u);
+                    const uint32_t tO = tmem + lane_sel + kJointO + 64 * s;
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32(tO + c * 32, o);
+                        tmem_wait_ld();
+                        tmem_loaded(o);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                        tmem_st32(tO + c * 32, o);
+                    }
+                    tmem_wait_st();
+                }
+                m = m_new;
+            }
+            const float neg_m = m == -INFINITY ? 0.f : kWeightShift - m;
+            const uint64_t neg_m_x2 = pack_f32x2(neg_m, neg_m);
+            uint64_t ex_a = 0ull, ex_b = 0ull;
+            uint32_t buf[2][32];
+            tmem_ld32(tMine, buf[0]);
+            tmem_ld32(tMine + 32, buf[1]);
+            tmem_wait_ld();
+            tmem_loaded(buf[0]);
+            tmem_loaded(buf[1]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float s0 = kscale[2 * c] * scale2, s1 = kscale[2 * c + 1] * scale2;
+                const uint64_t s0_x2 = pack_f32x2(s0, s0), s1_x2 = pack_f32x2(s1, s1);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    float x0, x1;
+                    const uint64_t xx = fma_f32x2(pack_f32x2(__uint_as_float(buf[c][2 * j]), __uint_as_float(buf[c][2 * j + 1])), j < 8 ? s0_x2 : s1_x2, neg_m_x2);
+                    unpack_f32x2(xx, x0, x1);
+                    const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+                    pk[c * 16 + j] = pack2_16bit<true>(p0, p1);
+                    const uint64_t pe = pack_f32x2(p0, p1);
+                    if (j & 1) ex_b = add_f32x2(ex_b, pe);
+                    else ex_a = add_f32x2(ex_a, pe);
+                }
+            }
+            float b0, b1;
+            unpack_f32x2(add_f32x2(ex_a, ex_b), b0, b1);
+            sum = b0 + b1;
+            // No weight can exceed the sum: one of at most 2^(8 + 7) means that no score is more than 2^8 above its reference.  All
+            // threads have read S when they meet here: P, which lies in S's first columns, may be stored.
+            if (!any_of(7, both, sum > kWeightLimit) || tries == 2) break;
+        }
+        tmem_st32(tS + 32 * s, pk);
+        l += sum;
+        tmem_wait_st();
+        tc_fence_before();
+        asm volatile("bar.arrive %0, %1;" ::"r"(9 + p_bar), "r"(both + 32) : "memory");      // hand-off of P, once per tile on every path
+        if (++b == 3u) b = 0;
+        if (++p_bar == 3u) p_bar = 0;
+    }
+    // an idle warp has seen none of the phases: they are what the others' are
+    if (idle)
+        for (int i = 0; i < T; ++i) { phases ^= 1u << b; if (++b == 3u) b = 0; }
+    // ---- segment end
+    k->sum[s][wtid] = l;
+    if (!idle) mbar_wait_certain(smem_u32(&aux->joint_o_done), done_phase & 1u, &aux->abort_flag);
+    tc_fence_after();
+    meet_before_segment(aux, js.seg_no + 1, js.leader);      // both warpgroups done: all MMAs of the segment have completed
+    const volatile Segment& again = aux->seg[js.seg_no % kSegs];
+    const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
+    const bool write_ok = !bad && !*const_cast<volatile int*>(&aux->abort_flag);
+    const long long part_base = (2ll * blockIdx.x + (js.seg_no > 0 ? 1 : 0)) * kPartialRows;
+    const int node = (int)row_node(p, rr);
+    const long long out_row = rr < again.M ? (long long)(again.node_base + node) * p.num_q_heads + again.h * G + (rr - node * G) : 0;
+    const bool row_ok = write_ok && rr < again.M, whole = again.tile0 == 0 && again.tile1 == again.tiles;
+    // staging for coalesced stores: Q is idle now
+    float* stage = reinterpret_cast<float*>(smem + (s * 4 + ((threadIdx.x >> 5) & 3)) * kStageBytesPerWarp);
+    const float lt = k->sum[0][wtid] + k->sum[1][wtid], w = lt > 0.f ? 1.f / lt : 0.f;
+    tc_fence_after();
+#pragma unroll 1
+    for (int c4 = 2 * s; c4 < (idle ? 0 : 2 * s + 2); ++c4) {
+        uint32_t o[32];
+        tmem_ld32(tmem + lane_sel + kJointO + c4 * 32, o);
+        tmem_wait_ld();
+        tmem_loaded(o);
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * w;
+        if (whole) store_rows32<kF16>(p, stage, out_row, row_ok, c4 * 32, v);
+        else if (row_ok) {
+            // a partial: [32 groups of four channels][rows][4]
+            float4* part = reinterpret_cast<float4*>(p.part_o) + part_base * 32 + rr;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) part[(c4 * 8 + j) * kPartialRows] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        }
+    }
+    if (s == 0 && rr < again.M) {
+        const float lse = lse_of_sum(m, lt);
+        if (!write_ok) {
+            if (bad && !whole) p.part_lse[part_base + rr] = __uint_as_float(kBadPartial);      // the merge leaves the row alone
+        } else if (!whole) p.part_lse[part_base + rr] = lse;
+        else if (p.lse) p.lse[out_row] = lse;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ joint units, keys on lanes
+// Thread = key of the tile, in both warpgroups; warpgroup s has kHalf of the unit's rows, from row s * kHalf on.  A row's numbers (scale,
+// reference) lie in shared memory and are the same for the warpgroup's four warps, which agree after each tile on whether all
+// scores stayed within the lazy threshold of their rows' references.  `sum`: the weights of pairs of rows over this thread's keys.
+template <int kHalf, bool kF16>
+struct KeysStream {
+    const AttnParams& p;
+    AuxFp8* aux;
+    KeysScratch* k;
+    uint32_t tmem, tS;               // tS: of the tile, this warp's lanes and this warpgroup's rows
+    unsigned char* p_row;            // this key's row of the tile's P, from this warpgroup's rows on
+    int s, wtid;
+    uint64_t sum[kHalf / 2];
+
+    static constexpr int kRows = 2 * kHalf;
+    __device__ __forceinline__ int row0() const { return s * kHalf; }
+    __device__ __forceinline__ void begin(const Segment& g) {
+        if (wtid < kHalf) {
+            const int row = row0() + wtid;
+            // rows beyond M: weights of 0; others: any score at all is above the threshold until the first reference is there
+            k->scale[row] = row < g.M ? p.sm_scale * 1.4426950408889634f * aux->row_scale[row] : 0.f;
+            k->bias[row] = row < g.M ? 1e30f : -INFINITY;
+            k->m[row] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < kHalf / 2; ++r) sum[r] = 0ull;
+        named_barrier(7 + s, 128);
+    }
+    // scores of 16 rows from the warpgroup's row `r0` on, without their scales: the pieces' columns added up
+    struct Columns { uint32_t a[kPieces<kF16>][16]; };
+    __device__ __forceinline__ void ask(int r0, Columns& c) {
+#pragma unroll
+        for (int piece = 0; piece < kPieces<kF16>; ++piece) tmem_ld16(tS + piece * kRows + r0, c.a[piece]);
+    }
+    __device__ __forceinline__ void add_up(Columns& c, uint64_t (&x)[8]) {
+#pragma unroll
+        for (int piece = 0; piece < kPieces<kF16>; ++piece) {
+            tmem_loaded(c.a[piece]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint64_t y = pack_f32x2(__uint_as_float(c.a[piece][2 * j]), __uint_as_float(c.a[piece][2 * j + 1]));
+                x[j] = piece == 0 ? y : add_f32x2(x[j], y);
+            }
+        }
+    }
+    // The tile reaches drafted positions (or the end of the sequence): what a row does not see gets a score of -inf, in tensor memory.  A slot
+    // past the end may have held a NaN, so all its pieces are replaced.
+    __device__ __forceinline__ void mask(const Segment& g, int t) {
+        const int j = t * kTileKeys + wtid - g.L;              // this key as a drafted node; below 0: context
+#pragma unroll 1
+        for (int r0 = 0; r0 < kHalf; r0 += 16) {
+            uint32_t sees = 0u;
+#pragma unroll 1
+            for (int r = 0; r < 16; ++r) {
+                const int row = row0() + r0 + r;
+                const bool yes = j < 0 || (row < g.M && j < kMaxNodes && (aux->anc[row_node(p, row)] >> j & 1ull));
+                sees |= yes ? 1u << r : 0u;
+            }
+#pragma unroll 1
+            for (int piece = 0; piece < kPieces<kF16>; ++piece) {
+                uint32_t a[16];
+                tmem_ld16(tS + piece * kRows + r0, a);
+                tmem_wait_ld();
+                tmem_loaded(a);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!(sees >> r & 1u)) a[r] = piece == 0 ? 0xff800000u : 0u;
+                tmem_st16(tS + piece * kRows + r0, a);
+            }
+        }
+        tmem_wait_st();
+    }
+    // Weights against the rows' references, to P and into `sum`; true if some score is above its reference by more than the
+    // threshold.  Weights stop at 2^15.5 (a NaN stays one), so that in that case they can be taken out of `sum` again (kBack; P is
+    // then written anew): what that leaves in it is 2^-24 of a sum that the new reference makes small.
+    template <bool kBack>
+    __device__ __forceinline__ bool weigh(float kscale) {
+        const uint64_t ks_x2 = pack_f32x2(kscale, kscale);
+        __half2 top = __float2half2_rn(0.f);
+        Columns col[kHalf / 16];
+#pragma unroll
+        for (int h = 0; h < kHalf / 16; ++h) ask(16 * h, col[h]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int h = 0; h < kHalf / 16; ++h) {
+            uint64_t x[8];
+            uint32_t pk[8];
+            add_up(col[h], x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const ulonglong2 sc = *reinterpret_cast<const ulonglong2*>(&k->scale[row0() + 16 * h + 4 * j]);
+                const ulonglong2 bi = *reinterpret_cast<const ulonglong2*>(&k->bias[row0() + 16 * h + 4 * j]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint64_t y = fma_f32x2(mul_f32x2(x[2 * j + i], i ? sc.y : sc.x), ks_x2, i ? bi.y : bi.x);
+                    float y0, y1;
+                    unpack_f32x2(y, y0, y1);
+                    const float p0 = fast_exp2(min_or_nan(y0, 15.5f)), p1 = fast_exp2(min_or_nan(y1, 15.5f));
+                    pk[2 * j + i] = pack2_16bit<true>(p0, p1);
+                    top = __hmax2(top, *reinterpret_cast<const __half2*>(&pk[2 * j + i]));
+                    uint64_t& to = sum[8 * h + 2 * j + i];
+                    to = add_f32x2(to, kBack ? pack_f32x2(-p0, -p1) : pack_f32x2(p0, p1));
+                }
+            }
+            if constexpr (!kBack) {
+                // P: keys' rows of 128 bytes, 16-byte piece c at place c ^ (key & 7); MN-major operand
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    *reinterpret_cast<uint4*>(p_row + (((row0() / 8 + 2 * h + c) ^ (wtid & 7)) << 4)) = make_uint4(pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
+            }
+        }
+        return __low2float(top) > kWeightLimit || __high2float(top) > kWeightLimit;
+    }
+    // The rows' references move up to the tile's largest scores.
+    __device__ __forceinline__ void raise(float kscale, bool first, uint32_t seq) {
+        const int lane = wtid & 31, warp = wtid >> 5;
+        unsigned most = 0u;                                    // lane i's: of the warpgroup's row i over the warp's keys
+#pragma unroll 1
+        for (int h = 0; h < kHalf; h += 16) {
+            uint64_t x[8];
+            Columns col;
+            ask(h, col);
+            tmem_wait_ld();
+            add_up(col, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float y[2];
+                unpack_f32x2(x[j], y[0], y[1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const unsigned u = __reduce_max_sync(0xffffffffu, ordered(y[i] * k->scale[row0() + h + 2 * j + i] * kscale));
+                    if (lane == h + 2 * j + i) most = u;
+                }
+            }
+        }
+        if (lane < kHalf) k->most[warp][row0() + lane] = most;
+        named_barrier(7 + s, 128);
+        bool moved = false;
+        if (wtid < kHalf) {
+            const int row = row0() + wtid;
+            const float m = k->m[row];
+            const float m_new = fmaxf(m, from_ordered(max(max(k->most[0][row], k->most[1][row]), max(k->most[2][row], k->most[3][row]))));
+            moved = k->bias[row] > -INFINITY && m_new > m;
+            k->alpha[row] = moved ? fast_exp2(m - m_new) : 1.f;
+            if (moved) { k->m[row] = m_new; k->bias[row] = kWeightShift - m_new; }
+        }
+        if (!any_of(7 + s, 128, moved) || first) return;       // (nothing has been added up yet)
+#pragma unroll
+        for (int r = 0; r < kHalf / 2; ++r) sum[r] = mul_f32x2(sum[r], pack_f32x2(k->alpha[row0() + 2 * r], k->alpha[row0() + 2 * r + 1]));
+        wait_for_product(aux, seq - 1u);
+        const uint32_t tO = tmem + kJointO + row0();
+#pragma unroll 1
+        for (int h = 0; h < kHalf; h += 16) {
+            uint32_t o[16];
+            tmem_ld16(tO + h, o);
+            tmem_wait_ld();
+            tmem_loaded(o);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * k->alpha[row0() + h + r]);
+            tmem_st16(tO + h, o);
+        }
+        tmem_wait_st();
+    }
+    __device__ __forceinline__ void tile(float kscale, bool first, uint32_t seq) {
+        if (!first) {
+            if (!any_of(7 + s, 128, weigh<false>(kscale))) return;
+            weigh<true>(kscale);
+        }
+        raise(kscale, first, seq);
+        weigh<false>(kscale);
+    }
+    // the sums over the keys: lane i of each warp leaves row i's over the warp
+    __device__ __forceinline__ void finish() {
+        const int lane = wtid & 31, warp = wtid >> 5;
+        float v[kHalf];
+#pragma unroll
+        for (int i = 0; i < kHalf / 2; ++i) unpack_f32x2(sum[i], v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int o = kHalf / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < o; ++i) {
+                const bool up = lane & o;
+                const float send = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+            }
+        if (kHalf == 16) v[0] += __shfl_xor_sync(0xffffffffu, v[0], 16);
+        if (lane < kHalf) k->sum[warp][row0() + lane] = v[0];
+    }
+};
+
+template <int kHalf, bool kWide, bool kF16>
+__device__ __forceinline__ void keys_segment(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s, const JointSegment& js,
+                                             uint32_t& phases, const uint32_t done_phase) {
+    constexpr int kRows = 2 * kHalf;
+    constexpr uint32_t kColumns = kPieces<kF16> * kRows;
+    const Segment& g = js.g;
+    const int wtid = threadIdx.x - 128 - s * 128;
+    const uint32_t lane_sel = (uint32_t)(((threadIdx.x >> 5) & 3) * 32) << 16;
+    KeysScratch* k = reinterpret_cast<KeysScratch*>(smem + kScratchOff<kWide, kF16>);
+    const int T = g.tile1 - g.tile0;
+    {
+        KeysStream<kHalf, kF16> ks{p, aux, k, tmem + lane_sel, 0u, nullptr, s, wtid, {}};
+        ks.begin(g);
+        uint32_t b = 0, p_bar = 0;
+        for (int i = 0; i < T; ++i) {
+            const int t = g.tile0 + i;
+            const uint32_t seq = js.tile_base + (uint32_t)i;
+            wait_for_scores(aux, b, phases);
+            if (i >= 2) wait_for_product(aux, seq - 2u);           // the last reader of this P
+            ks.tS = tmem + lane_sel + joint_s(b, kColumns) + s * kHalf;
+            ks.p_row = smem + kPOff<kF16> + (i & 1) * kPBytes + wtid * 128;
+            if ((t + 1) * kTileKeys > g.L) ks.mask(g, t);
+            ks.tile(aux->note[seq % kNotes].kscale[wtid >> 4], i == 0, seq);
+            fence_proxy_async_smem();                  // P is read by the product
+            tc_fence_before();
+            asm volatile("bar.arrive %0, 288;" ::"r"(9 + p_bar) : "memory");      // hand-off of P, once per tile on every path
+            if (++b == joint_buffers(kColumns)) b = 0;
+            if (++p_bar == 3u) p_bar = 0;
+        }
+        ks.finish();
+    }
+    mbar_wait_certain(smem_u32(&aux->joint_o_done), done_phase & 1u, &aux->abort_flag);
+    tc_fence_after();
+    meet_before_segment(aux, js.seg_no + 1, js.leader);    // both warpgroups done: all MMAs of the segment have completed
+    const volatile Segment& again = aux->seg[js.seg_no % kSegs];
+    const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
+    const bool write_ok = !bad && !*const_cast<volatile int*>(&aux->abort_flag);
+    const long long part_base = (2ll * blockIdx.x + (js.seg_no > 0 ? 1 : 0)) * kPartialRows;
+    const int M = again.M, node_base = again.node_base, h = again.h, G = p.group;
+    const bool whole = again.tile0 == 0 && again.tile1 == again.tiles;
+    tc_fence_after();
+    auto out_row_of = [&](int row) {
+        const int node = (int)row_node(p, row);
+        return (long long)(node_base + node) * p.num_q_heads + h * G + (row - node * G);
+    };
+    if (wtid < kHalf) {
+        const int row = s * kHalf + wtid;
+        const float l = (k->sum[0][row] + k->sum[1][row]) + (k->sum[2][row] + k->sum[3][row]);
+        k->w[row] = l > 0.f ? 1.f / l : 0.f;
+        if (row < M) {
+            if (write_ok) {
+                const float lse = lse_of_sum(k->m[row], l);
+                if (!whole) p.part_lse[part_base + row] = lse;
+                else if (p.lse) p.lse[out_row_of(row)] = lse;
+            } else if (bad && !whole) {
+                p.part_lse[part_base + row] = __uint_as_float(kBadPartial);      // the merge leaves the row alone
+            }
+        }
+    }
+    named_barrier(7 + s, 128);
+    // Lane = channel: a warp's 32 channels of a row are neighbours.
+#pragma unroll 1
+    for (int r0 = s * kHalf; r0 < s * kHalf + kHalf; r0 += 16) {
+        uint32_t o[16];
+        tmem_ld16(tmem + lane_sel + kJointO + r0, o);
+        tmem_wait_ld();
+        tmem_loaded(o);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = r0 + r;
+            if (!write_ok || row >= M) continue;
+            const float v = __uint_as_float(o[r]) * k->w[row];
+            if (whole) reinterpret_cast<uint16_t*>(p.out)[out_row_of(row) * kHeadDim + wtid] = (uint16_t)pack2_16bit<kF16>(v, 0.f);
+            else p.part_o[(part_base * 32 + (long long)(wtid >> 2) * kPartialRows + row) * 4 + (wtid & 3)] = v;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ shared units
+// The weights of a tile against the running maximum m, 32 columns of S at a time.  False, with nothing stored, if some
 // row's weights show that a score may exceed m by more than the lazy threshold (`force`: this row's do).
 __device__ __forceinline__ bool weigh_tile(const uint32_t tS, const float* kscale, const float scale2, const float m, float& l, bool& force) {
     const uint64_t neg_m_x2 = pack_f32x2(kWeightShift - m, kWeightShift - m);
@@ -489,325 +980,181 @@ __device__ __forceinline__ bool weigh_tile(const uint32_t tS, const float* kscal
     return true;
 }
 
-// log-sum-exp of a row from its reference and its sum of shifted weights (a NaN sum stays one)
-__device__ __forceinline__ float lse_of_sum(float m, float sum) {
-    return sum > 0.f ? (m - kWeightShift + __log2f(sum)) * 0.6931471805599453f : sum == 0.f ? -INFINITY : sum;
-}
-__device__ __forceinline__ unsigned ordered(float x) {        // sorts like x; a NaN is below everything
-    const unsigned u = __float_as_uint(x);
-    return x != x ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-__device__ __forceinline__ float from_ordered(unsigned u) { return u == 0u ? -INFINITY : __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
-__device__ __forceinline__ float min_or_nan(float x, float y) {
-    float r;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
-    return r;
-}
-// Meets the calling stream's 128 threads; true for all if it is for one.
-__device__ __forceinline__ bool any_of_stream(int s, bool mine) {
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
-                 : "=r"(r) : "r"(7 + s), "r"(mine ? 1u : 0u) : "memory");
-    return r != 0;
-}
-
-// What the products of a stream wait for besides P, looked at before P is announced by two of the warps that announce it: the first waits
-// until V of tile `seq` has been turned into fp16, the second until the stream's next K tile has landed (`next`).  The MMA warp then waits
-// on a hardware barrier alone (25 clocks if it is late; a look at an mbarrier is 100 to 190, and it is the MMA warp whose instructions
-// a tile waits for).  A wait that gives up raises the abort flag; P is announced all the same.
-template <uint32_t kPlaces>
-__device__ __forceinline__ void tiles_for_products(AuxFp8* aux, uint32_t seq, bool next, int wtid, volatile int* abort_flag) {
-    if (wtid < 32) mbar_wait(smem_u32(&aux->v_full[seq % kFp8VSlots]), (seq / kFp8VSlots) & 1u, abort_flag);
-    else if (wtid < 64 && next) mbar_wait(smem_u32(&aux->raw_full[2u * ((seq + 2u) % kPlaces)]), ((seq + 2u) / kPlaces) & 1u, abort_flag);
-    __syncwarp();
-}
-
-// ------------------------------------------------------------------------------------------ keys on lanes
-// A stream's key tiles of one segment.  Thread = key of the tile; kRows = the unit's rows, padded.  A row's numbers (scale, reference) lie in
-// shared memory and are the same for the stream's four warps, which agree after each tile on whether all scores stayed
-// within the lazy threshold of their rows' references.  `sum[r]`: the weights of row r over this thread's keys.
-template <int kRows, bool kF16>
-struct KeysStream {
-    const AttnParams& p;
-    AuxFp8* aux;
-    KeysScratch* k;
-    unsigned char* p_tile;           // this stream's P
-    uint32_t tS, tO;
-    int s, wtid;
-    uint64_t sum[kRows / 2];         // pairs of rows
-
-    __device__ __forceinline__ void begin(const Segment& g) {
-        if (wtid < kRows) {
-            // rows beyond M: weights of 0; others: any score at all is above the threshold until the first reference is there
-            k->scale[s][wtid] = wtid < g.M ? p.sm_scale * 1.4426950408889634f * aux->row_scale[wtid] : 0.f;
-            k->bias[s][wtid] = wtid < g.M ? 1e30f : -INFINITY;
-            k->m[s][wtid] = -INFINITY;
-        }
-#pragma unroll
-        for (int r = 0; r < kRows / 2; ++r) sum[r] = 0ull;
-        named_barrier(7 + s, 128);
-    }
-    // scores of 16 rows from `r0` on, without their scales: the pieces' columns added up
-    __device__ __forceinline__ void scores(int r0, uint64_t (&x)[8]) {
-        uint32_t a[kPieces<kF16>][16];
-#pragma unroll
-        for (int piece = 0; piece < kPieces<kF16>; ++piece) tmem_ld16(tS + piece * kRows + r0, a[piece]);
-        tmem_wait_ld();
-#pragma unroll
-        for (int piece = 0; piece < kPieces<kF16>; ++piece) {
-            tmem_loaded(a[piece]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint64_t y = pack_f32x2(__uint_as_float(a[piece][2 * j]), __uint_as_float(a[piece][2 * j + 1]));
-                x[j] = piece == 0 ? y : add_f32x2(x[j], y);
-            }
-        }
-    }
-    // The tile reaches drafted positions (or the end of the sequence): what a row does not see gets a score of -inf, in tensor memory.  A slot
-    // past the end may have held a NaN, so all its pieces are replaced.
-    __device__ __forceinline__ void mask(const Segment& g, int t) {
-        const int j = t * kTileKeys + wtid - g.L;              // this key as a drafted node; below 0: context
-#pragma unroll 1
-        for (int r0 = 0; r0 < kRows; r0 += 32) {
-            uint32_t sees = 0u;
-#pragma unroll 1
-            for (int r = 0; r < 32; ++r) {
-                const int row = r0 + r;
-                const bool yes = j < 0 || (row < g.M && j < kMaxNodes && (aux->anc[row_node(p, row)] >> j & 1ull));
-                sees |= yes ? 1u << r : 0u;
-            }
-#pragma unroll 1
-            for (int piece = 0; piece < kPieces<kF16>; ++piece) {
-                uint32_t a[32];
-                tmem_ld32(tS + piece * kRows + r0, a);
-                tmem_wait_ld();
-                tmem_loaded(a);
-#pragma unroll
-                for (int r = 0; r < 32; ++r)
-                    if (!(sees >> r & 1u)) a[r] = piece == 0 ? 0xff800000u : 0u;
-                tmem_st32(tS + piece * kRows + r0, a);
-            }
-        }
-        tmem_wait_st();
-    }
-    // Weights of 32 rows from r0 on against their references, to P and into `sum`; true if some score is above its reference by more than the
-    // threshold.  Weights stop at 2^15.5 (a NaN stays one), so that in that case they can be taken out of `sum` again (kBack; P is
-    // then written anew): what that leaves in it is 2^-24 of a sum that the new reference makes small.
-    template <int r0, bool kBack>
-    __device__ __forceinline__ bool weigh(float kscale) {
-        const uint64_t ks_x2 = pack_f32x2(kscale, kscale);
-        __half2 top = __float2half2_rn(0.f);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint64_t x[8];
-            uint32_t pk[8];
-            scores(r0 + 16 * h, x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const ulonglong2 sc = *reinterpret_cast<const ulonglong2*>(&k->scale[s][r0 + 16 * h + 4 * j]);
-                const ulonglong2 bi = *reinterpret_cast<const ulonglong2*>(&k->bias[s][r0 + 16 * h + 4 * j]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint64_t y = fma_f32x2(mul_f32x2(x[2 * j + i], i ? sc.y : sc.x), ks_x2, i ? bi.y : bi.x);
-                    float y0, y1;
-                    unpack_f32x2(y, y0, y1);
-                    const float p0 = fast_exp2(min_or_nan(y0, 15.5f)), p1 = fast_exp2(min_or_nan(y1, 15.5f));
-                    pk[2 * j + i] = pack2_16bit<true>(p0, p1);
-                    top = __hmax2(top, *reinterpret_cast<const __half2*>(&pk[2 * j + i]));
-                    uint64_t& to = sum[r0 / 2 + 8 * h + 2 * j + i];
-                    to = add_f32x2(to, kBack ? pack_f32x2(-p0, -p1) : pack_f32x2(p0, p1));
-                }
-            }
-            if constexpr (!kBack) {
-                // P: keys' rows of 128 bytes, 16-byte piece c at place c ^ (key & 7); MN-major operand
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    *reinterpret_cast<uint4*>(p_tile + (((r0 / 8 + 2 * h + c) ^ (wtid & 7)) << 4)) = make_uint4(pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
-            }
-        }
-        return __low2float(top) > kWeightLimit || __high2float(top) > kWeightLimit;
-    }
-    // The references of 32 rows move up to the tile's largest scores where those are above them (force) or above the threshold.
-    template <int r0>
-    __device__ __forceinline__ void raise(float kscale, bool force, bool first) {
-        if (wtid < 32) k->most[s][wtid] = 0u;
-        named_barrier(7 + s, 128);
-#pragma unroll 1
-        for (int h = 0; h < 32; h += 16) {
-            uint64_t x[8];
-            scores(r0 + h, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float y[2];
-                unpack_f32x2(x[j], y[0], y[1]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const unsigned u = __reduce_max_sync(0xffffffffu, ordered(y[i] * k->scale[s][r0 + h + 2 * j + i] * kscale));
-                    if ((wtid & 31) == 0) atomicMax(&k->most[s][h + 2 * j + i], u);
-                }
-            }
-        }
-        named_barrier(7 + s, 128);
-        bool moved = false;
-        if (wtid < 32) {
-            const int row = r0 + wtid;
-            const float m = k->m[s][row], m_new = fmaxf(m, from_ordered(k->most[s][wtid]));
-            const bool real = k->bias[s][row] > -INFINITY;
-            moved = real && (force || first ? m_new > m : m_new - m > kLazyRescale);
-            k->alpha[s][wtid] = moved ? fast_exp2(m - m_new) : 1.f;
-            if (moved) { k->m[s][row] = m_new; k->bias[s][row] = kWeightShift - m_new; }
-        }
-        if (!any_of_stream(s, moved) || first) return;         // (nothing has been added up yet)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum[r0 / 2 + r] = mul_f32x2(sum[r0 / 2 + r], pack_f32x2(k->alpha[s][2 * r], k->alpha[s][2 * r + 1]));
-        // S of this tile is here, and the commit that announced it covers the product before it: O may be touched
-        tc_fence_after();
-#pragma unroll 1
-        for (int h = 0; h < 32; h += 16) {
-            uint32_t o[16];
-            tmem_ld16(tO + r0 + h, o);
-            tmem_wait_ld();
-            tmem_loaded(o);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * k->alpha[s][h + r]);
-            tmem_st16(tO + r0 + h, o);
-        }
-        tmem_wait_st();
-    }
-    template <int r0>
-    __device__ __forceinline__ void rows32(float kscale, bool first) {
-        bool force = false;
-        if (!first) {
-            force = any_of_stream(s, weigh<r0, false>(kscale));
-            if (!force) return;
-            weigh<r0, true>(kscale);
-        }
-        raise<r0>(kscale, force, first);
-        weigh<r0, false>(kscale);
-    }
-    // the sums over the stream's keys: lane i of each warp leaves row i's (then row 32 + i's) over the warp
-    __device__ __forceinline__ void finish() {
-        const int lane = wtid & 31, warp = wtid >> 5;
-#pragma unroll
-        for (int r0 = 0; r0 < kRows; r0 += 32) {
-            float v[32];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) unpack_f32x2(sum[r0 / 2 + i], v[2 * i], v[2 * i + 1]);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-                for (int i = 0; i < o; ++i) {
-                    const bool up = lane & o;
-                    const float send = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
-                    v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
-                }
-            k->sum[s][warp][r0 + lane] = v[0];
-        }
-    }
-};
-
-// The key loop and the results of a segment with keys on lanes; `it`, `tile_base`: the stream's S tiles and the CTA's key tiles so far.
-template <int kRows, bool kWide, bool kF16>
-__device__ __forceinline__ void keys_segment(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s, const Segment& g,
-                                             const uint32_t it, const uint32_t od_phase, const uint32_t tile_base, const uint32_t seg_no, const bool leader) {
-    const int wtid = threadIdx.x - 128 - s * 128;
+// Stream s has rows [128 s, 128 s + 128); `it`: S tiles of the CTA's earlier shared segments.
+template <bool kF16>
+__device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s, const JointSegment& js,
+                                               const uint32_t it, const uint32_t od_phase) {
+    constexpr uint32_t kPlaces = kRawTiles<true, kF16>;
+    const Segment& g = js.g;
+    const int wtid = threadIdx.x - 128 - s * 128, G = p.group;
     volatile int* abort_flag = &aux->abort_flag;
     const uint32_t lane_sel = (uint32_t)(((threadIdx.x >> 5) & 3) * 32) << 16;
-    constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
-    KeysScratch* k = reinterpret_cast<KeysScratch*>(smem + kScratchOff<kWide, kF16>);
-    const int n_it = g.iters(s);
-    {
-        KeysStream<kRows, kF16> ks{p, aux, k, smem + kPOff<kF16> + s * kPBytes + wtid * 128, tmem + lane_sel + s * kKeysS,
-                                   tmem + lane_sel + kKeysO + s * 64, s, wtid, {}};
-        ks.begin(g);
-        for (int i = 0; i < n_it; ++i) {
-            const int t = g.tile(s, i);
-            mbar_wait_certain(smem_u32(&aux->s_full[s]), (it + i) & 1u, abort_flag);
-            tc_fence_after();
-            const float kscale = aux->note[(tile_base + (uint32_t)(t - g.tile0)) % kNotes].kscale[wtid >> 4];
-            if ((t + 1) * kTileKeys > g.L) ks.mask(g, t);
-            ks.template rows32<0>(kscale, i == 0);
-            if constexpr (kRows == 64) ks.template rows32<32>(kscale, i == 0);
-            tiles_for_products<kPlaces>(aux, tile_base + (uint32_t)(t - g.tile0), i + 1 < n_it, wtid, abort_flag);
-            fence_proxy_async_smem();                  // P is read by the product
-            tc_fence_before();
-            asm volatile("bar.arrive %0, 160;" ::"r"(4 + s) : "memory");      // hand-off of P, once per tile on every path
+    const uint32_t tS = tmem + lane_sel + s * 128, tO = tS + 256;
+    const int rr = s * 128 + wtid, T = g.tile1 - g.tile0;
+    const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
+    const float scale2 = p.sm_scale * 1.4426950408889634f * aux->row_scale[rr];
+    float m = -INFINITY, l = 0.f;
+    for (int i = 0; i < T; ++i) {
+        const int t = g.tile0 + i;
+        const uint32_t seq = js.tile_base + (uint32_t)i;
+        mbar_wait_certain(smem_u32(&aux->s_full[s]), (it + i) & 1u, abort_flag);
+        tc_fence_after();
+        const float* kscale = aux->note[seq % kNotes].kscale;
+        if ((t + 1) * kTileKeys > g.L) {
+            // the mask of the drafted positions (rows_segment), over 128 keys
+            const int j0 = t * kTileKeys - g.L;
+            unsigned long long lo, hi;
+            if (j0 >= 0) {
+                lo = j0 < 64 ? anc_row >> j0 : 0ull;
+                hi = 0ull;
+            } else {
+                const int k = -j0;   // 1..127 prefix keys at the front of the tile
+                if (k >= 64) { lo = ~0ull; hi = (k == 64 ? 0ull : (~0ull >> (128 - k))) | (anc_row << (k - 64)); }
+                else { lo = (~0ull >> (64 - k)) | (anc_row << k); hi = anc_row >> (64 - k); }
+            }
+#pragma unroll 1
+            for (int c4 = 0; c4 < 4; ++c4) {
+                const uint32_t bits = (uint32_t)((c4 < 2 ? lo : hi) >> ((c4 & 1) * 32));
+                uint32_t r[32];
+                tmem_ld32(tS + c4 * 32, r);
+                tmem_wait_ld();
+                tmem_loaded(r);
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (!((bits >> j) & 1u)) r[j] = 0xff800000u;   // -inf
+                tmem_st32(tS + c4 * 32, r);
+            }
+            tmem_wait_st();
         }
-        ks.finish();
+        bool done = false, force = false;
+        if (i > 0 && !__any_sync(0xffffffffu, m == -INFINITY)) done = weigh_tile(tS, kscale, scale2, m, l, force);
+        if (!done) {
+            // The long way: the tile's maximum first, then the weights; twice over tensor memory and rolled, because
+            // it runs on a segment's first tile and after a jump of the maximum only.
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int c4 = 0; c4 < 4; ++c4) {
+                uint32_t r[32];
+                tmem_ld32(tS + c4 * 32, r);
+                tmem_wait_ld();
+                tmem_loaded(r);
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    float a = __uint_as_float(r[16 * hf]);
+#pragma unroll
+                    for (int j = 1; j < 16; ++j) a = fmaxf(a, __uint_as_float(r[16 * hf + j]));
+                    mx = fmaxf(mx, a * (kscale[2 * c4 + hf] * scale2));
+                }
+            }
+            const float m_new = fmaxf(m, mx);
+            // (false when both are -inf: NaN compares false)  A tile sent here by the fast path's sum moves m up at once.
+            const bool need = force ? m_new > m : (m_new - m) > kLazyRescale;
+            if (__any_sync(0xffffffffu, need)) {
+                const float alpha = (m_new == -INFINITY) ? 1.f : fast_exp2(m - m_new);
+                if (i > 0) {
+                    // S of this tile is here, and its product was issued after O += P V of the tile before: the
+                    // commit that announced S covers that product too, so O may be touched now
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c4 = 0; c4 < 4; ++c4) {
+                        uint32_t o[32];
+                        tmem_ld32(tO + c4 * 32, o);
+                        tmem_wait_ld();
+                        tmem_loaded(o);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                        tmem_st32(tO + c4 * 32, o);
+                    }
+                    tmem_wait_st();
+                    l *= alpha;
+                }
+                m = m_new;
+            }
+            const float neg_m = (m == -INFINITY) ? 0.f : kWeightShift - m;
+            float sum = 0.f;
+#pragma unroll 1
+            for (int c4 = 0; c4 < 4; ++c4) {
+                // the weights of 32 keys take columns that hold only scores already read (16 c4 + 16 <= 32 (c4 + 1))
+                uint32_t sv[32], pk[16];
+                tmem_ld32(tS + c4 * 32, sv);
+                tmem_wait_ld();
+                tmem_loaded(sv);
+                float x_a = 0.f, x_b = 0.f;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float sc = kscale[2 * c4 + (j >> 3)] * scale2;
+                    const float p0 = fast_exp2(fmaf(__uint_as_float(sv[2 * j]), sc, neg_m)), p1 = fast_exp2(fmaf(__uint_as_float(sv[2 * j + 1]), sc, neg_m));
+                    pk[j] = pack2_16bit<true>(p0, p1);
+                    x_a += p0; x_b += p1;
+                }
+                tmem_st16(tS + c4 * 16, pk);
+                sum += x_a + x_b;
+            }
+            l += sum;
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        // V of the tile has been turned into fp16 (stream 1's product follows stream 0's).  A wait that gives up raises the abort flag; the
+        // arrivals happen all the same.
+        if (s == 0 && wtid < 32) {
+            mbar_wait(smem_u32(&aux->v_full[seq % kFp8VSlots]), (seq / kFp8VSlots) & 1u, abort_flag);
+            __syncwarp();
+        }
+        // Hand-off of P on hardware barrier 4 + s, once per key tile of this stream, on every path (softmax_loop)
+        asm volatile("bar.arrive %0, 160;" ::"r"(4 + s) : "memory");
+        // the next K tile has landed (hardware barrier 6, T - 1 times; softmax_loop)
+        if (s == 0 && wtid < 32 && i + 1 < T) {
+            mbar_wait(smem_u32(&aux->raw_full[2u * ((seq + 1u) % kPlaces)]), ((seq + 1u) / kPlaces) & 1u, abort_flag);
+            __syncwarp();
+            asm volatile("bar.arrive 6, 64;" ::: "memory");
+        }
     }
-    if (n_it > 0) mbar_wait_certain(smem_u32(&aux->o_done[s]), od_phase & 1u, abort_flag);
+    // ---- segment end: every product of this stream has completed
+    mbar_wait_certain(smem_u32(&aux->o_done[s]), od_phase & 1u, abort_flag);
     tc_fence_after();
-    meet_before_segment(aux, seg_no + 1, leader);    // both streams done: all MMAs of the segment have completed
-    const volatile Segment& again = aux->seg[seg_no % kSegs];
+    meet_before_segment(aux, js.seg_no + 1, js.leader);    // both streams done: all MMAs of the segment have completed
+    const volatile Segment& again = aux->seg[js.seg_no % kSegs];
     const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
     const bool write_ok = !bad && !*abort_flag;
-    const long long part_base = (2ll * blockIdx.x + (seg_no > 0 ? 1 : 0)) * kRowsOfPartial;
-    const int M = again.M, node_base = again.node_base, h = again.h, G = p.group;
-    const bool whole = again.tile0 == 0 && again.tile1 == again.tiles;
-    const bool use_b = g.iters(1) > 0;
+    const long long part_base = (2ll * blockIdx.x + (js.seg_no > 0 ? 1 : 0)) * kPartialRows;
+    const int node = (int)row_node(p, rr);
+    const long long out_row = rr < again.M ? (long long)(again.node_base + node) * p.num_q_heads + again.h * G + (rr - node * G) : 0;
+    const bool row_ok = write_ok && rr < again.M, whole = again.tile0 == 0 && again.tile1 == again.tiles;
+    float* stage = reinterpret_cast<float*>(smem + (s * 4 + ((threadIdx.x >> 5) & 3)) * kStageBytesPerWarp);
+    const float w = l > 0.f ? 1.f / l : 0.f;
     tc_fence_after();
-    auto out_row_of = [&](int row) {
-        const int node = (int)row_node(p, row);
-        return (long long)(node_base + node) * p.num_q_heads + h * G + (row - node * G);
-    };
-    if (s == 0 && wtid < kRows) {
-        const int row = wtid;
-        float l[2];
+#pragma unroll 1
+    for (int c4 = 0; c4 < 4; ++c4) {
+        uint32_t o[32];
+        tmem_ld32(tO + c4 * 32, o);
+        tmem_wait_ld();
+        tmem_loaded(o);
+        float v[32];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) l[b] = (k->sum[b][0][row] + k->sum[b][1][row]) + (k->sum[b][2][row] + k->sum[b][3][row]);
-        const float m0 = k->m[0][row], m1 = k->m[1][row], mm = fmaxf(m0, m1);
-        const float a0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - mm), a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mm);
-        const float lt = a0 * l[0] + a1 * l[1], inv = lt > 0.f ? 1.f / lt : 0.f;
-        k->w[0][row] = a0 * inv;
-        k->w[1][row] = a1 * inv;
-        if (row < M) {
-            if (write_ok) {
-                const float lse = lse_of_sum(mm, lt);
-                if (!whole) p.part_lse[part_base + row] = lse;
-                else if (p.lse) p.lse[out_row_of(row)] = lse;
-            } else if (bad && !whole) {
-                p.part_lse[part_base + row] = __uint_as_float(kBadPartial);      // the merge leaves the row alone
-            }
+        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * w;
+        if (whole) store_rows32<kF16>(p, stage, out_row, row_ok, c4 * 32, v);
+        else if (row_ok) {
+            float4* part = reinterpret_cast<float4*>(p.part_o) + part_base * 32 + rr;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) part[(c4 * 8 + j) * kPartialRows] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         }
     }
-    named_barrier(1, 256);
-    // Lane = channel.  Each warpgroup writes 16 rows of every 32, and a warp's 32 channels of a row are neighbours.
-#pragma unroll 1
-    for (int r0 = 16 * s; r0 < kRows; r0 += 32) {
-        uint32_t oa[16], ob[16];
-        tmem_ld16(tmem + lane_sel + kKeysO + r0, oa);
-        if (use_b) tmem_ld16(tmem + lane_sel + kKeysO + 64 + r0, ob);
-        tmem_wait_ld();
-        tmem_loaded(oa);
-        tmem_loaded(ob);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = r0 + r;
-            float v = __uint_as_float(oa[r]) * k->w[0][row];
-            if (use_b) v = fmaf(__uint_as_float(ob[r]), k->w[1][row], v);
-            if (!write_ok || row >= M) continue;
-            if (whole) {
-                const uint32_t u = pack2_16bit<kF16>(v, 0.f);
-                reinterpret_cast<uint16_t*>(p.out)[out_row_of(row) * kHeadDim + wtid] = (uint16_t)u;
-            } else {
-                // a partial: [32 groups of four channels][rows][4]
-                p.part_o[(part_base * 32 + (long long)(wtid >> 2) * kRowsOfPartial + row) * 4 + (wtid & 3)] = v;
-            }
-        }
+    if (rr < again.M) {
+        const float lse = lse_of_sum(m, l);
+        if (!write_ok) {
+            if (bad && !whole) p.part_lse[part_base + rr] = __uint_as_float(kBadPartial);
+        } else if (!whole) p.part_lse[part_base + rr] = lse;
+        else if (p.lse) p.lse[out_row] = lse;
     }
 }
 
+// ------------------------------------------------------------------------------------------ softmax warpgroups
 template <bool kWide, bool kF16>
-__device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s /*stream*/) {
-    constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
+__device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s /*warpgroup*/) {
     const int wtid = threadIdx.x - 128 - s * 128;          // 0..127 inside the warpgroup; TMEM lane
-    volatile int* abort_flag = &aux->abort_flag;
-    const uint32_t lane_sel = (uint32_t)(((threadIdx.x >> 5) & 3) * 32) << 16;
-    const uint32_t tS = tmem + lane_sel + s * 128;
-    const int G = p.group;
-    uint32_t it = 0, seg_no = 0, od_phase = 0;   // od_phase: segments of this stream that issued a product
-    uint32_t tile_base = 0;                      // key tiles of the CTA's earlier segments
-
+    uint32_t seg_no = 0, tile_base = 0;          // segments and key tiles so far
+    uint32_t phases = 0, joint_segs = 0;         // joint units: phases of the S buffers' barriers, segments
+    uint32_t shared_it = 0, shared_segs = 0;     // shared units: tiles, segments
     const bool leader = s == 0 && wtid < 32;
     meet_before_segment(aux, 0, leader);
     for (;;) {
@@ -819,7 +1166,7 @@ __device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* au
         if (seg_no > 0) named_barrier(1, 256);   // the other warpgroup may still be reading its staging area in the Q block
         if (leader) const_cast<volatile int&>(aux->seg_reached) = (int)seg_no;
         {
-            // rows on lanes, 256 rows: a block of 128 rows for each warpgroup; else each loads half of the rows
+            // shared: a block of 128 rows for each warpgroup; else each loads half of the rows
             const int half = keys ? keys >> 1 : 64, r_in_8 = wtid >> 4;
             const int first = g.shared ? r_in_8 : half * s + r_in_8;
             load_q_fp8<kF16>(p, g, aux, smem + (g.shared ? s * kPieces<kF16> * kPieceBytes : 0) + first * 128, keys ? keys * 128 : kPieceBytes,
@@ -848,238 +1195,16 @@ __device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* au
         named_barrier(1, 256);                 // masks and the tree verdict are visible to both warpgroups
         mbar_arrive(smem_u32(&aux->q_full));
 
-        const int n_it = g.iters(s);
-        if (keys) {
-            if (keys == 32) keys_segment<32, kWide, kF16>(p, aux, smem, tmem, s, g, it, od_phase, tile_base, seg_no, leader);
-            else keys_segment<64, kWide, kF16>(p, aux, smem, tmem, s, g, it, od_phase, tile_base, seg_no, leader);
-            it += (uint32_t)n_it;
-            if (n_it > 0) ++od_phase;
-            tc_fence_before();
-            tile_base += (uint32_t)(g.tile1 - g.tile0);
-            ++seg_no;
-            continue;
-        }
-        const int rr = (g.shared ? s * 128 : 0) + wtid;            // packed row of this thread
-        const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
-        const float scale2 = p.sm_scale * 1.4426950408889634f * aux->row_scale[rr];
-        const int live = kWide ? 4 : live_warps_fp8(g.M);
-        const bool idle = (wtid >> 5) >= live;       // no row of the unit in this warp: straight to the segment's end
-        float m = -INFINITY, l = 0.f;
-
-        for (int i = 0; i < (idle ? 0 : n_it); ++i) {
-            const int t = g.tile(s, i);
-            mbar_wait_certain(smem_u32(&aux->s_full[s]), (it + i) & 1u, abort_flag);
-            tc_fence_after();
-            const float* kscale = aux->note[(tile_base + (uint32_t)(t - g.tile0)) % kNotes].kscale;
-            if ((t + 1) * kTileKeys > g.L) {
-                // The tile reaches drafted positions (or the end of the sequence): at most two tiles per unit.
-                // Visibility of its 128 keys for this row: prefix keys all, drafted key j iff ancestor-or-self.
-                // The mask is applied to S in tensor memory, 32 columns at a time, before the common path reads it.
-                const int j0 = t * kTileKeys - g.L;
-                unsigned long long lo, hi;
-                if (j0 >= 0) {
-                    lo = j0 < 64 ? anc_row >> j0 : 0ull;
-                    hi = 0ull;
-                } else {
-                    const int k = -j0;   // 1..127 prefix keys at the front of the tile
-                    if (k >= 64) { lo = ~0ull; hi = (k == 64 ? 0ull : (~0ull >> (128 - k))) | (anc_row << (k - 64)); }
-                    else { lo = (~0ull >> (64 - k)) | (anc_row << k); hi = anc_row >> (64 - k); }
-                }
-#pragma unroll 1
-                for (int c4 = 0; c4 < 4; ++c4) {
-                    const uint32_t bits = (uint32_t)((c4 < 2 ? lo : hi) >> ((c4 & 1) * 32));
-                    uint32_t r[32];
-                    tmem_ld32(tS + c4 * 32, r);
-                    tmem_wait_ld();
-                    tmem_loaded(r);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (!((bits >> j) & 1u)) r[j] = 0xff800000u;   // -inf
-                    tmem_st32(tS + c4 * 32, r);
-                }
-                tmem_wait_st();
-            }
-            bool done = false, force = false;
-            if (i > 0 && !__any_sync(0xffffffffu, m == -INFINITY)) {
-                done = weigh_tile(tS, kscale, scale2, m, l, force);
-            }
-            if (!done) {
-                // The long way: the tile's maximum first, then the weights; twice over tensor memory and rolled, because
-                // it runs on a segment's first tile and after a jump of the maximum only.
-                float mx = -INFINITY;
-#pragma unroll 1
-                for (int c4 = 0; c4 < 4; ++c4) {
-                    uint32_t r[32];
-                    tmem_ld32(tS + c4 * 32, r);
-                    tmem_wait_ld();
-                    tmem_loaded(r);
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        float a = __uint_as_float(r[16 * hf]);
-#pragma unroll
-                        for (int j = 1; j < 16; ++j) a = fmaxf(a, __uint_as_float(r[16 * hf + j]));
-                        mx = fmaxf(mx, a * (kscale[2 * c4 + hf] * scale2));
-                    }
-                }
-                const float m_new = fmaxf(m, mx);
-                // (false when both are -inf: NaN compares false)  A tile sent here by the fast path's sum moves m up at once.
-                const bool need = force ? m_new > m : (m_new - m) > kLazyRescale;
-                if (__any_sync(0xffffffffu, need)) {
-                    const float alpha = (m_new == -INFINITY) ? 1.f : fast_exp2(m - m_new);
-                    if (i > 0) {
-                        // S of this tile is here, and its product was issued after O += P V of the tile before: the
-                        // commit that announced S covers that product too, so O may be touched now
-                        tc_fence_after();
-                        const uint32_t tO = tmem + lane_sel + 256 + s * 128;
-#pragma unroll 1
-                        for (int c4 = 0; c4 < 4; ++c4) {
-                            uint32_t o[32];
-                            tmem_ld32(tO + c4 * 32, o);
-                            tmem_wait_ld();
-                            tmem_loaded(o);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                            tmem_st32(tO + c4 * 32, o);
-                        }
-                        tmem_wait_st();
-                        l *= alpha;
-                    }
-                    m = m_new;
-                }
-                const float neg_m = (m == -INFINITY) ? 0.f : kWeightShift - m;
-                float sum = 0.f;
-#pragma unroll 1
-                for (int c4 = 0; c4 < 4; ++c4) {
-                    // the weights of 32 keys take columns that hold only scores already read (16 c4 + 16 <= 32 (c4 + 1))
-                    uint32_t sv[32], pk[16];
-                    tmem_ld32(tS + c4 * 32, sv);
-                    tmem_wait_ld();
-                    tmem_loaded(sv);
-                    float x_a = 0.f, x_b = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float sc = kscale[2 * c4 + (j >> 3)] * scale2;
-                        const float p0 = fast_exp2(fmaf(__uint_as_float(sv[2 * j]), sc, neg_m)), p1 = fast_exp2(fmaf(__uint_as_float(sv[2 * j + 1]), sc, neg_m));
-                        pk[j] = pack2_16bit<true>(p0, p1);
-                        x_a += p0; x_b += p1;
-                    }
-                    tmem_st16(tS + c4 * 16, pk);
-                    sum += x_a + x_b;
-                }
-                l += sum;
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            // (both streams on one tile: stream 1's product follows stream 0's)
-            if (!g.shared) tiles_for_products<kPlaces>(aux, tile_base + (uint32_t)(t - g.tile0), i + 1 < n_it, wtid, abort_flag);
-            else if (kWide && s == 0) tiles_for_products<kPlaces>(aux, tile_base + (uint32_t)i, false, wtid, abort_flag);
-            // Hand-off of P on hardware barrier 4 + s, once per key tile of this stream, on every path (softmax_loop)
-            asm volatile("bar.arrive %0, %1;" ::"r"(4 + s), "r"(32 * live + 32) : "memory");
-            // Units of more than 128 rows: the next K tile has landed (hardware barrier 6, T - 1 times; softmax_loop)
-            if (kWide && g.shared && s == 0 && wtid < 32 && i + 1 < n_it) {
-                const uint32_t seq = tile_base + (uint32_t)(i + 1);
-                mbar_wait(smem_u32(&aux->raw_full[2u * (seq % kPlaces)]), (seq / kPlaces) & 1u, abort_flag);
-                __syncwarp();
-                asm volatile("bar.arrive 6, 64;" ::: "memory");
-            }
-        }
-        it += (uint32_t)n_it;
-
-        // ---- segment end: every product of this stream has completed
-        // (an idle warp sleeps on the hardware barrier below instead; it touches no tensor memory)
-        if (n_it > 0) {
-            if (!idle) mbar_wait_certain(smem_u32(&aux->o_done[s]), od_phase & 1u, abort_flag);
-            ++od_phase;
-        }
-        tc_fence_after();
-        // both streams on the same rows: they exchange (m, l) through the first columns of their S (softmax_loop)
-        if (!g.shared && !idle) {
-            const uint32_t mine[4] = {__float_as_uint(m), __float_as_uint(l), 0u, 0u};
-            tmem_st4(tS, mine);
-            tmem_wait_st();
-            tc_fence_before();
-        }
-        meet_before_segment(aux, seg_no + 1, leader);    // both streams done: all MMAs of the segment have completed
-        const volatile Segment& again = aux->seg[seg_no % kSegs];
-        const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
-        const bool write_ok = !bad && !*abort_flag;
-        // only the first and the last unit of a CTA's piece can be cut: two partial slots per CTA
-        const long long part_base = (2ll * blockIdx.x + (seg_no > 0 ? 1 : 0)) * kRows;
-        const int M = again.M, node_base = again.node_base, h = again.h;
-        auto out_row_of = [&](int row) {
-            const int node = (int)row_node(p, row);
-            return (long long)(node_base + node) * p.num_q_heads + h * G + (row - node * G);
-        };
-        const bool row_ok = write_ok && rr < M;
-        const bool whole = again.tile0 == 0 && again.tile1 == again.tiles;
-        // staging for coalesced stores: Q is idle now (every MMA of the segment is done)
-        float* stage = reinterpret_cast<float*>(smem + (s * 4 + ((threadIdx.x >> 5) & 3)) * kStageBytesPerWarp);
-        // a partial: [32 groups of four channels][kRows rows][4]
-        float4* part_o = reinterpret_cast<float4*>(p.part_o) + part_base * 32;
-        float wa, wb = 0.f, lse;
-        uint32_t tOa = tmem + lane_sel + 256 + s * 128, tOb = tmem + lane_sel + 384;
-        bool use_b = false, write_lse = true;
-        int c_first = 0, c_count = 4;
-        if (g.shared) {
-            wa = l > 0.f ? 1.f / l : 0.f;
-            lse = lse_of_sum(m, l);
+        const JointSegment js{g, tile_base, seg_no, leader};
+        if (kWide && g.shared) {
+            shared_segment<kF16>(p, aux, smem, tmem, s, js, shared_it, shared_segs);
+            shared_it += (uint32_t)(g.tile1 - g.tile0);
+            ++shared_segs;
         } else {
-            // (a stream without a tile has m = -inf and nothing in its sums)
-            use_b = g.iters(1) > 0;
-            float m0 = m, l0 = l, m1 = m, l1 = l;
-            uint32_t st[4];
-            tc_fence_after();
-            if (!idle && (kWide || s == 1)) {
-                tmem_ld4(tmem + lane_sel, st);
-                tmem_wait_ld();
-                tmem_loaded(st);
-                m0 = __uint_as_float(st[0]); l0 = __uint_as_float(st[1]);
-            }
-            if (!idle && (kWide || s == 0)) {
-                tmem_ld4(tmem + lane_sel + 128, st);
-                tmem_wait_ld();
-                tmem_loaded(st);
-                m1 = __uint_as_float(st[0]); l1 = __uint_as_float(st[1]);
-            }
-            const float mm = fmaxf(m0, m1);
-            const float a0 = (m0 == -INFINITY) ? 0.f : fast_exp2(m0 - mm);
-            const float a1 = (m1 == -INFINITY) ? 0.f : fast_exp2(m1 - mm);
-            const float lt = a0 * l0 + a1 * l1;
-            const float inv = lt > 0.f ? 1.f / lt : 0.f;
-            wa = a0 * inv; wb = a1 * inv;
-            lse = lse_of_sum(mm, lt);
-            tOa = tmem + lane_sel + 256;
-            write_lse = s == 0;
-            c_first = 2 * s; c_count = 2;
-        }
-        if (idle) c_count = 0;
-#pragma unroll 1
-        for (int c4 = c_first; c4 < c_first + c_count; ++c4) {
-            uint32_t oa[32], ob[32];
-            tmem_ld32(tOa + c4 * 32, oa);
-            if (use_b) tmem_ld32(tOb + c4 * 32, ob);
-            tmem_wait_ld();
-            tmem_loaded(oa);
-            tmem_loaded(ob);
-            float v[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                v[j] = __uint_as_float(oa[j]) * wa;           // rows that saw no key have O = 0 and weight 0
-                if (use_b) v[j] = fmaf(__uint_as_float(ob[j]), wb, v[j]);
-            }
-            if (whole) {
-                store_rows32<kF16>(p, stage, rr < M ? out_row_of(rr) : 0, row_ok, c4 * 32, v);
-            } else if (row_ok) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    part_o[(c4 * 8 + j) * kRows + rr] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-            }
-        }
-        if (row_ok && write_lse) {
-            if (whole) { if (p.lse) p.lse[out_row_of(rr)] = lse; }
-            else p.part_lse[part_base + rr] = lse;
-        } else if (bad && write_lse && !whole && rr < M) {
-            p.part_lse[part_base + rr] = __uint_as_float(kBadPartial);      // the merge leaves the row alone
+            if (keys == 32) keys_segment<16, kWide, kF16>(p, aux, smem, tmem, s, js, phases, joint_segs);
+            else if (keys) keys_segment<32, kWide, kF16>(p, aux, smem, tmem, s, js, phases, joint_segs);
+            else rows_segment<kWide, kF16>(p, aux, smem, tmem, s, js, phases, joint_segs);
+            ++joint_segs;
         }
         tc_fence_before();
         tile_base += (uint32_t)(g.tile1 - g.tile0);
@@ -1106,6 +1231,8 @@ verify_attn_fp8_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k
                 mbar_init(smem_u32(&aux->raw_full[2 * i + kv]), 2);            // the bytes and the note
                 mbar_init(smem_u32(&aux->raw_empty[2 * i + kv]), kv ? 4 : 1);  // V: the converting warps; K: the products
             }
+        for (int i = 0; i < 3; ++i) mbar_init(smem_u32(&aux->joint_s_full[i]), 1);
+        mbar_init(smem_u32(&aux->joint_o_done), 1);
         for (int i = 0; i < kFp8VSlots; ++i) {
             mbar_init(smem_u32(&aux->v_full[i]), 4);
             mbar_init(smem_u32(&aux->v_empty[i]), 1);
