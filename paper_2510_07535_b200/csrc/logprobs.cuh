@@ -2,12 +2,13 @@
 //
 // One pass over the logits, in two kernels:
 //   logprob_scan_kernel   a warp takes a (row, vocabulary chunk) item, 32 logits per lane and round, the next round's loads in
-//                         flight meanwhile.  Per lane m = running maximum, s = sum e^(x - m), t = sum e^(x - m) (x - m);
-//                         per warp the chunk's best tokens, one per lane, sorted.
-//   logprob_merge_kernel  a CTA per row joins the chunks:  lse = m + ln s,  entropy = ln s - t / s,  and scores a token.
-// Bound by the logits' bytes: per element a maximum, a subtraction, a product, a clamp, an ex2 and two sums.
-// The list costs little because it is looked at only in rounds with a logit above its last entry: in the first round that limit is
-// taken from the lanes' maxima (at least `top` logits are not below the top-th largest of them), later it only rises.
+//                         flight meanwhile.  Per lane m = running maximum, s = sum e^(x - m), t = sum e^(x - m) (x - m); and, where
+//                         alternatives are asked for, each lane's maximum of each round is left in a table: one for 32 logits.
+//   logprob_merge_kernel  a CTA per row joins the chunks:  lse = m + ln s,  entropy = ln s - t / s,  scores a token, and finds
+//                         the alternatives: of 64 maxima over parts of the table the top-th largest is not above the top-th
+//                         largest logit, so the groups of 32 whose maximum reaches it hold all of them, some tens of groups.
+// Bound by the logits' bytes: per element a maximum, a subtraction, a product, a clamp, an ex2 and two sums.  (A sorted list per warp in the
+// scan instead of the table: 256 rows of 128256 fp32 logits 42.8 us with 20 alternatives and 23.9 without, 8 rows 13.9 and 2.7.)
 #pragma once
 
 #include "accept.cuh"
@@ -15,7 +16,7 @@
 
 namespace owl {
 
-constexpr int kMaxTop = 32;              // alternatives per row: one per lane
+constexpr int kMaxTop = 32;              // alternatives per row
 constexpr int kScoreWarps = 8;
 constexpr int kScoreRound = 1024;        // logits per warp and round
 constexpr int kScoreMaxChunk = 16384;
@@ -34,61 +35,18 @@ struct ScoreParams {
     int32_t* top_ids;                    // [N, top]
     float* top_logprobs;
     ScorePartial* part;                  // [N, chunks]
-    unsigned long long* part_keys;       // [N, chunks, top], descending
+    float* maxima;                       // [N, chunks, rounds + 1, 32]: of each lane's logits of a round; last, up to 16 ragged logits
     float2* row_sums;                    // [N] a row's (m, s), for the rows of later launches of the call; null: there are none
     int32_t* status;
-    int32_t batch, total_nodes, nodes_uniform, max_nodes, vocab, top, chunk, chunks;
+    int32_t batch, total_nodes, nodes_uniform, max_nodes, vocab, top, chunk, chunks, rounds;
     int32_t row0, rows;                  // this launch's rows [row0, row0 + rows); the partials are counted from row0
 };
 
-// What an entry of the list is ordered by: larger logit first, then the lower token.  0: no entry (-inf and NaN make none).
+// What alternatives are ordered by: larger logit first, then the lower token.  0: none (-inf and NaN make none).
 __device__ __forceinline__ unsigned long long score_key(float x, uint32_t idx) { return x > -INFINITY ? argmax_key(x, idx) : 0ull; }
 __device__ __forceinline__ float key_logit(unsigned long long key) {
     const uint32_t u = (uint32_t)(key >> 32);
     return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
-}
-__device__ __forceinline__ unsigned long long shfl_key(unsigned long long k, int lane) { return __shfl_sync(0xffffffffu, k, lane); }
-
-// Two descending lists of 32 (one entry per lane) to the descending list of the 32 largest: the larger of a[i] and b[31 - i] are
-// those, in a bitonic order, which five exchanges sort.
-__device__ __forceinline__ unsigned long long merge_lists(unsigned long long a, unsigned long long b) {
-    const int lane = threadIdx.x & 31;
-    const unsigned long long r = shfl_key(b, 31 - lane);
-    a = a > r ? a : r;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const unsigned long long other = __shfl_xor_sync(0xffffffffu, a, o);
-        const bool larger = (lane & o) == 0;
-        a = (other > a) == larger ? other : a;
-    }
-    return a;
-}
-// One key per lane, in any order, to a descending list (bitonic sort).
-__device__ __forceinline__ unsigned long long sort_list(unsigned long long a) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-        for (int o = size >> 1; o > 0; o >>= 1) {
-            const unsigned long long other = __shfl_xor_sync(0xffffffffu, a, o);
-            const bool larger = ((lane & o) == 0) == ((lane & size) == 0);
-            a = (other > a) == larger ? other : a;
-        }
-    return a;
-}
-// `mine`: a candidate per lane, 0 for none.  A few go in one by one, more are sorted and merged.
-__device__ __forceinline__ unsigned long long join_list(unsigned long long list, unsigned long long mine) {
-    const int lane = threadIdx.x & 31;
-    unsigned from = __ballot_sync(0xffffffffu, mine != 0ull);
-    if (__popc(from) > 6) return merge_lists(list, sort_list(mine));
-    while (from) {
-        const unsigned long long k = shfl_key(mine, __ffs(from) - 1);
-        from &= from - 1;
-        const int at = __popc(__ballot_sync(0xffffffffu, list > k));
-        const unsigned long long up = __shfl_up_sync(0xffffffffu, list, 1);
-        list = lane < at ? list : lane == at ? k : up;
-    }
-    return list;
 }
 
 __device__ __forceinline__ float exp_of(float d) { return fast_exp2(d * 1.4426950408889634f); }
@@ -142,12 +100,9 @@ __device__ __forceinline__ void score_unpack(const ScoreLoad<T>& l, float (&x)[3
     }
 }
 
-// A lane's sums and the warp's list while it works through a chunk.
+// A lane's sums while its warp works through a chunk.
 struct ScoreState {
     float m = -INFINITY, s = 0.f, t = 0.f;
-    unsigned long long list = 0ull;
-    float limit = -INFINITY;             // a logit must be above it to enter the list
-    bool full = false;                   // the list has `top` entries
 };
 // The lane's logits of a round (absent ones: -inf).
 template <int kCount>
@@ -172,73 +127,45 @@ __device__ __forceinline__ void score_sums(ScoreState& st, const float (&x)[kCou
     st.s += s0 + s1;
     st.t += t0 + t1;
 }
-// Candidates of a round, one per lane at a time.  `at(i)`: the token of the lane's i-th logit; within a lane they ascend, and every
-// token of an earlier round is lower than any of this one, so a logit equal to the limit cannot enter.
-template <int kCount, typename At>
-__device__ __forceinline__ void score_list(ScoreState& st, int top, const float (&x)[kCount], float round_max, At at) {
-    constexpr unsigned kAll = 0xffffffffu;
-    float limit = st.limit;
-    if (!st.full) {
-        // At least `top` logits are not below the top-th largest of the lanes' maxima, so what is below cannot enter; what
-        // equals it may: the limit is the next smaller number.
-        int above = 0;
-#pragma unroll 8
-        for (int o = 0; o < 32; ++o) {
-            const float other = __shfl_sync(kAll, round_max, o);
-            above += other > round_max || (other == round_max && o < (int)(threadIdx.x & 31));
-        }
-        const unsigned who = __ballot_sync(kAll, above == top - 1);
-        const float edge = __shfl_sync(kAll, round_max, who ? __ffs(who) - 1 : 0);
-        if (who && edge > -INFINITY) {
-            const uint32_t u = __float_as_uint(edge + 0.f);
-            limit = edge == 0.f ? -1.4e-45f : __uint_as_float(edge > 0.f ? u - 1u : u + 1u);
-        }
+// The parts of a chunk: [c0, a0) up to 16-byte alignment, [a0, a1) whole loads, [a1, c1) the rest.
+template <typename T>
+struct ScoreChunk {
+    const T* row;
+    long long c0, c1, a0, a1;
+    __device__ __forceinline__ ScoreChunk(const ScoreParams& p, long long at_row, int chunk) {
+        row = static_cast<const T*>(p.logits) + at_row * p.vocab;
+        c0 = (long long)chunk * p.chunk;
+        c1 = min((long long)p.vocab, c0 + p.chunk);
+        const uintptr_t addr = reinterpret_cast<uintptr_t>(row + c0);
+        a0 = min(c1, c0 + (long long)(((16 - (addr & 15)) & 15) / sizeof(T)));
+        a1 = a0 + (c1 - a0) / ScoreLoad<T>::kPer * ScoreLoad<T>::kPer;
     }
-    if (!__any_sync(kAll, round_max > limit)) return;
-    uint32_t mine = 0u;
-#pragma unroll
-    for (int i = 0; i < kCount; ++i) mine |= x[i] > limit ? 1u << i : 0u;
-    while (__any_sync(kAll, mine != 0u)) {
-        const int i = mine ? __ffs(mine) - 1 : 0;
-        // the i-th of the lane's registers
-        float v = x[0];
-#pragma unroll
-        for (int j = 1; j < kCount; ++j) v = i == j ? x[j] : v;
-        unsigned long long key = mine ? score_key(v, at(i)) : 0ull;
-        mine &= mine - 1u;
-        key = key > shfl_key(st.list, top - 1) ? key : 0ull;
-        st.list = join_list(st.list, key);
+    // the token of a ragged logit, `i` of 16: the first eight before a0, the others from a1 on; -1: there is none
+    __device__ __forceinline__ long long ragged(int i) const {
+        const long long v = i < 8 ? c0 + i : a1 + (i - 8);
+        return i < 16 && v < (i < 8 ? a0 : c1) ? v : -1;
     }
-    const unsigned long long last = shfl_key(st.list, top - 1);
-    st.full = last != 0ull;
-    st.limit = st.full ? key_logit(last) : -INFINITY;
-}
+};
 
 template <typename T, bool kTop>
 __device__ __forceinline__ void score_chunk_warp(const ScoreParams& p, const int row, const int chunk, const long long item) {
     constexpr int kPer = ScoreLoad<T>::kPer, kLoads = ScoreLoad<T>::kLoads;
     const int lane = threadIdx.x & 31;
-    const long long V = p.vocab;
-    const long long c0 = (long long)chunk * p.chunk, c1 = min(V, c0 + p.chunk);
-    const T* base = static_cast<const T*>(p.logits) + (p.row0 + row) * V;
-    // [c0, a0) up to 16-byte alignment, [a0, a1) whole loads, [a1, c1) the rest
-    const uintptr_t addr = reinterpret_cast<uintptr_t>(base + c0);
-    long long a0 = c0 + (long long)(((16 - (addr & 15)) & 15) / sizeof(T));
-    if (a0 > c1) a0 = c1;
-    const long long a1 = a0 + (c1 - a0) / kPer * kPer;
-    const uint4* body = reinterpret_cast<const uint4*>(base + a0);
-    const int nvec = (int)((a1 - a0) / kPer);
+    const ScoreChunk<T> c(p, p.row0 + row, chunk);
+    const uint4* body = reinterpret_cast<const uint4*>(c.row + c.a0);
+    const int nvec = (int)((c.a1 - c.a0) / kPer);
     const uint64_t policy = l2_evict_first_policy();      // the logits are read once
     constexpr float kNone = -INFINITY;
+    float* maxima = kTop ? p.maxima + item * (p.rounds + 1) * 32 + lane : nullptr;
 
     ScoreState st;
-    auto ragged = [&](long long from, long long to) {      // at most seven logits, one per lane
-        if (from >= to) return;
-        float x[1] = {from + lane < to ? score_of(base[from + lane]) : kNone};
+    {
+        const long long v = c.ragged(lane);
+        float x[1] = {v >= 0 ? score_of(c.row[v]) : kNone};
         const float mx = fmaxf(x[0], kNone);
         score_sums(st, x, mx);
-        if constexpr (kTop) score_list(st, p.top, x, mx, [&](int) { return (uint32_t)(from + lane); });
-    };
+        if constexpr (kTop) maxima[p.rounds * 32] = mx;
+    }
     auto load = [&](int v0, ScoreLoad<T>& l) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
@@ -258,25 +185,24 @@ __device__ __forceinline__ void score_chunk_warp(const ScoreParams& p, const int
         for (int j = 0; j < 8; ++j) g[j] = fmaxf(fmaxf(x[4 * j], x[4 * j + 1]), fmaxf(x[4 * j + 2], x[4 * j + 3]));
         const float mx = fmaxf(fmaxf(fmaxf(fmaxf(g[0], g[1]), fmaxf(g[2], g[3])), fmaxf(fmaxf(g[4], g[5]), fmaxf(g[6], g[7]))), kNone);
         score_sums(st, x, mx);
-        if constexpr (kTop)
-            score_list(st, p.top, x, mx, [&](int i) { return (uint32_t)(a0 + (long long)(v0 + (i / kPer) * 32 + lane) * kPer + i % kPer); });
+        if constexpr (kTop) maxima[v0 / (32 * kLoads) * 32] = mx;
     };
-    ragged(c0, a0);
     constexpr int kVecs = 32 * kLoads;       // per round
     ScoreLoad<T> la, lb;
     if (nvec > 0) load(0, la);
-    for (int v0 = 0; v0 < nvec; v0 += 2 * kVecs) {
+    int v0 = 0;
+    for (; v0 < nvec; v0 += 2 * kVecs) {
         if (v0 + kVecs < nvec) load(v0 + kVecs, lb);
         take(v0, la);
         if (v0 + 2 * kVecs < nvec) load(v0 + 2 * kVecs, la);
         if (v0 + kVecs < nvec) take(v0 + kVecs, lb);
     }
-    ragged(a1, c1);
+    if constexpr (kTop)
+        for (int r = (nvec + kVecs - 1) / kVecs; r < p.rounds; ++r) maxima[r * 32] = kNone;      // rounds that the last chunk has not
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         join_sums(st.m, st.s, st.t, __shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.t, o));
     if (lane == 0) *reinterpret_cast<float4*>(p.part + item) = make_float4(st.m, st.s, st.t, 0.f);
-    if (kTop && lane < p.top) p.part_keys[item * p.top + lane] = st.list;
 }
 
 template <typename T, bool kTop>
@@ -336,55 +262,170 @@ __device__ __forceinline__ int score_parent_row(const ScoreParams& p, int node) 
     return parent >= 0 && parent < node - lo ? lo + parent : -2;
 }
 
-// grid = rows.  Warps join the chunks' lists, then the first joins theirs; the second warp scores the row's token.
+// Largest of a CTA's keys; every thread gets it (two barriers).
+__device__ __forceinline__ unsigned long long largest_key(unsigned long long k, unsigned long long* s_keys /*[kScoreWarps]*/) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, k, o);
+        k = other > k ? other : k;
+    }
+    if ((threadIdx.x & 31) == 0) s_keys[threadIdx.x >> 5] = k;
+    __syncthreads();
+    k = s_keys[0];
+#pragma unroll
+    for (int w = 1; w < kScoreWarps; ++w) k = s_keys[w] > k ? s_keys[w] : k;
+    __syncthreads();
+    return k;
+}
+
+// grid = rows.  The first warp joins the chunks' sums, the second scores the row's token, and all look for the alternatives.
+constexpr int kScoreGroups = 512, kScoreCandidates = 1024;
+static_assert(kMaxTop <= kScoreWarps * 8, "as many parts of the table as alternatives");
 template <typename T>
 __global__ void __launch_bounds__(kScoreWarps * 32) logprob_merge_kernel(const ScoreParams p) {
-    __shared__ unsigned long long s_list[kScoreWarps][32];
+    constexpr int kThreads = kScoreWarps * 32, kPer = ScoreLoad<T>::kPer, kLoads = ScoreLoad<T>::kLoads;
+    __shared__ float s_max[kThreads / 4], s_edge, s_m, s_log_s;
+    __shared__ int s_groups[kScoreGroups], s_count[2];
+    __shared__ unsigned long long s_keys[kScoreCandidates];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int row = p.row0 + blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    unsigned long long list = 0ull;
+    const int row = p.row0 + blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int per_chunk = (p.rounds + 1) * 32, groups = p.chunks * per_chunk;      // < 2^31: the table's row fits the context
+    const float* maxima = p.maxima + (long long)blockIdx.x * groups;
+    // A thread holds its first 32 groups' maxima (8192 groups: all of a row of 200000 logits); the few beyond are read twice.
+    constexpr int kHeld = 32;
+    float held[kHeld];
     if (p.top > 0) {
-        const unsigned long long* keys = p.part_keys + (long long)blockIdx.x * p.chunks * p.top;
-        for (int c = warp; c < p.chunks; c += kScoreWarps) {
-            const unsigned long long k = lane < p.top ? __ldcg(keys + (long long)c * p.top + lane) : 0ull;
-            list = c == warp ? k : merge_lists(list, k);
-        }
-        if (warp > 0) s_list[warp][lane] = list;
-        __syncthreads();
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) held[i] = tid + i * kThreads < groups ? __ldcg(maxima + tid + i * kThreads) : -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) mx = fmaxf(mx, held[i]);
+#pragma unroll 8
+        for (int g = tid + kHeld * kThreads; g < groups; g += kThreads) mx = fmaxf(mx, __ldcg(maxima + g));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        if ((tid & 3) == 0) s_max[tid >> 2] = mx;
+        if (tid < 2) s_count[tid] = 0;
     }
     if (warp == 0) {
-        for (int w = 1; w < min(kScoreWarps, p.chunks) && p.top > 0; ++w) list = merge_lists(list, s_list[w][lane]);
         float m, s, t;
         score_row(p, row, m, s, t);
         const float log_s = score_log_s(m, s);
         if (lane == 0) {
+            s_m = m; s_log_s = log_s;
             if (p.row_sums) p.row_sums[row] = make_float2(m, s);
             if (p.lse) p.lse[row] = m == -INFINITY ? -INFINITY : m + log_s;
             if (p.entropy) p.entropy[row] = m == -INFINITY ? 0.f : log_s - t / s;
         }
-        if (lane < p.top) {
-            if (p.top_ids) p.top_ids[(long long)row * p.top + lane] = list ? (int)~(uint32_t)list : -1;
-            if (p.top_logprobs) p.top_logprobs[(long long)row * p.top + lane] = list ? score_logprob(key_logit(list), m, log_s) : -INFINITY;
-        }
     }
     if (warp == 1 && p.logprob) {
         const int token = p.tokens[row], from = p.tree_parent ? score_parent_row(p, row) : row;
-        if (from == -2) { if (lane == 0) report(p.status, kErrBadTree); return; }      // the row's logprob stays unwritten
-        float y = 0.f;                             // a root, or no token: nothing is scored
-        if (from >= 0 && token >= 0) {
-            y = -INFINITY;                         // a token that the vocabulary does not have
-            if (token < p.vocab) {
-                const float x = score_of(static_cast<const T*>(p.logits)[(long long)from * p.vocab + token]);
-                float m, s, t;
-                if (from < p.row0) {               // a row of an earlier launch (parents come first)
-                    const float2 sums = __ldcg(p.row_sums + from);
-                    m = sums.x; s = sums.y;
-                } else score_row(p, from, m, s, t);
-                y = x != x ? -INFINITY : score_logprob(x, m, score_log_s(m, s));
+        if (from == -2) {                          // this logprob stays unwritten
+            if (lane == 0) report(p.status, kErrBadTree);
+        } else {
+            float y = 0.f;                         // a root, or no token: nothing is scored
+            if (from >= 0 && token >= 0) {
+                y = -INFINITY;                     // a token that the vocabulary does not have
+                if (token < p.vocab) {
+                    const float x = score_of(static_cast<const T*>(p.logits)[(long long)from * p.vocab + token]);
+                    float m, s, t;
+                    if (from < p.row0) {           // a row of an earlier launch (parents come first)
+                        const float2 sums = __ldcg(p.row_sums + from);
+                        m = sums.x; s = sums.y;
+                    } else score_row(p, from, m, s, t);
+                    y = x != x ? -INFINITY : score_logprob(x, m, score_log_s(m, s));
+                }
+            }
+            if (lane == 0) p.logprob[row] = y;
+        }
+    }
+    if (p.top == 0) return;
+    __syncthreads();
+    if (tid < kThreads / 4) {
+        // the top-th largest of 64 maxima, four threads' each: at least `top` logits are not below it
+        const float mine = s_max[tid];
+        int above = 0;
+#pragma unroll
+        for (int j = 0; j < kThreads / 4; j += 4) {
+            const float4 o = *reinterpret_cast<const float4*>(s_max + j);
+            above += (o.x > mine || (o.x == mine && j < tid)) + (o.y > mine || (o.y == mine && j + 1 < tid)) +
+                     (o.z > mine || (o.z == mine && j + 2 < tid)) + (o.w > mine || (o.w == mine && j + 3 < tid));
+        }
+        if (above == p.top - 1) s_edge = mine;
+    }
+    __syncthreads();
+    const float edge = s_edge;
+    auto reaches = [&](float x) { return x >= edge && x > -INFINITY; };
+    auto take_group = [&](int g) {
+        const int at = atomicAdd(&s_count[0], 1);
+        if (at < kScoreGroups) s_groups[at] = g;
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if (reaches(held[i])) take_group(tid + i * kThreads);
+#pragma unroll 8
+    for (int g = tid + kHeld * kThreads; g < groups; g += kThreads)
+        if (reaches(__ldcg(maxima + g))) take_group(g);
+    __syncthreads();
+    const int found = s_count[0];
+    if (found <= kScoreGroups) {
+        // a group's logits lie in kLoads pieces of 16 bytes, 512 bytes apart: a thread per piece
+        for (int u = tid; u < found * kLoads; u += kThreads) {
+            const int g = s_groups[u / kLoads], j = u % kLoads;
+            const int chunk = g / per_chunk, r = g % per_chunk / 32, l = g % 32;
+            const ScoreChunk<T> c(p, row, chunk);
+            auto offer = [&](long long v, float x) {
+                if (reaches(x)) {
+                    const int at = atomicAdd(&s_count[1], 1);
+                    if (at < kScoreCandidates) s_keys[at] = score_key(x, (uint32_t)v);
+                }
+            };
+            if (r == p.rounds) {
+                const long long v = c.ragged(l);
+                if (j == 0 && v >= 0) offer(v, score_of(c.row[v]));
+            } else {
+                const long long v = c.a0 + ((long long)(r * kLoads + j) * 32 + l) * kPer;
+                if (v < c.a1) {
+                    const uint4 piece = *reinterpret_cast<const uint4*>(c.row + v);
+                    const T* x = reinterpret_cast<const T*>(&piece);
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) offer(v + e, score_of(x[e]));
+                }
             }
         }
-        if (lane == 0) p.logprob[row] = y;
+    }
+    __syncthreads();
+    const int count = s_count[1];
+    const float m = s_m, log_s = s_log_s;
+    auto write = [&](int j, unsigned long long k) {
+        if (p.top_ids) p.top_ids[(long long)row * p.top + j] = k ? (int)~(uint32_t)k : -1;
+        if (p.top_logprobs) p.top_logprobs[(long long)row * p.top + j] = k ? score_logprob(key_logit(k), m, log_s) : -INFINITY;
+    };
+    if (found <= kScoreGroups && count <= kScoreCandidates) {
+        // a candidate's place is the number of larger ones (their order here, which is by chance, does not matter)
+        for (int i = tid; i < max(count, p.top); i += kThreads) {
+            if (i >= count) { write(i, 0ull); continue; }
+            const unsigned long long mine = s_keys[i];
+            int above = 0;
+#pragma unroll 8
+            for (int j = 0; j < count; ++j) above += s_keys[j] > mine;
+            if (above < p.top) write(above, mine);
+        }
+    } else {
+        // hundreds of logits equal to the last one's value: one alternative after the other from the whole row
+        const T* logits = static_cast<const T*>(p.logits) + (long long)row * p.vocab;
+        unsigned long long last = ~0ull;
+        for (int j = 0; j < p.top; ++j) {
+            unsigned long long best = 0ull;
+            for (int v = tid; v < p.vocab; v += kThreads) {
+                const unsigned long long k = score_key(score_of(logits[v]), (uint32_t)v);
+                if (k < last && k > best) best = k;
+            }
+            best = largest_key(best, s_keys);
+            if (tid == 0) write(j, best);
+            last = best;
+        }
     }
 }
 
@@ -394,15 +435,24 @@ __global__ void __launch_bounds__(kScoreWarps * 32) logprob_merge_kernel(const S
 inline int score_chunk(long long rows, int vocab, int sms, long long most) {
     constexpr long long kItemCost = 700;
     const long long warps = (long long)sms * kScoreCtasPerSm * kScoreWarps;
-    int best = kScoreMaxChunk;
+    const long long whole = ((long long)vocab + kScoreRound - 1) / kScoreRound * kScoreRound;      // the row in one chunk
+    const int largest = whole < kScoreMaxChunk ? (int)whole : kScoreMaxChunk;
+    int best = largest;
     long long least = -1;
-    for (int chunk = kScoreRound; chunk <= kScoreMaxChunk; chunk += kScoreRound) {
+    for (int chunk = kScoreRound; chunk <= largest; chunk += kScoreRound) {
         const long long items = rows * (((long long)vocab + chunk - 1) / chunk);
         if (items > most) continue;
         const long long cost = (items + warps - 1) / warps * ((chunk < vocab ? chunk : vocab) + kItemCost);
         if (least < 0 || cost < least) { least = cost; best = chunk; }
     }
     return best;
+}
+// Places of a row's table of maxima, in chunks of `chunk`; what a context has room for: its largest call's in the smallest chunks, but no more
+// than 16 MB unless one row needs them.
+inline long long score_table(int vocab, int chunk) { return ((long long)vocab + chunk - 1) / chunk * (chunk / kScoreRound + 1) * 32; }
+inline long long score_table_room(long long rows, int vocab) {
+    const long long row = score_table(vocab, kScoreRound), want = rows * row, most = 4ll << 20;
+    return want < most ? want : row > most ? row : most;
 }
 // Items that a context has room for: those of its largest call in chunks of half the largest size, but no more than `kScoreMostItems` (a larger
 // call takes its rows in turns) and no less than two for each resident warp.

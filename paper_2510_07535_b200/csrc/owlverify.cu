@@ -41,10 +41,10 @@ struct owl_ctx {
     unsigned long long* part_keys = nullptr;
     unsigned long long* lm_keys = nullptr;      // KeySets: two sets of one arg-max key per row, then the call numbers
     long long part_keys_len = 0;
-    ScorePartial* score_part = nullptr;         // owl_token_logprobs: sums and lists of its (row, chunk) items, the rows' sums
-    unsigned long long* score_keys = nullptr;
+    ScorePartial* score_part = nullptr;         // owl_token_logprobs: sums of its (row, chunk) items, the rows' sums, groups' maxima
     float2* score_rows = nullptr;
-    long long score_len = 0;                    // items
+    float* score_maxima = nullptr;
+    long long score_len = 0, score_maxima_len = 0;
     // tensor maps over the callers' K and V caches: a few most recently used (cache pointers, geometry) pairs
     // are kept, so that a caller rotating over several caches does not pay two encodes per call
     EncodeTiledFn encode = nullptr;
@@ -332,8 +332,9 @@ int owl_create(owl_ctx** out, int device, const owl_dims* max_dims) {
         if (ok) ok = cudaMemset(ctx->lm_keys, 0, lm_bytes) == cudaSuccess;
         ctx->score_len = score_room(max_dims->total_nodes, max_dims->vocab, ctx->sm_count);
         alloc((void**)&ctx->score_part, (size_t)ctx->score_len * sizeof(ScorePartial));
-        alloc((void**)&ctx->score_keys, (size_t)ctx->score_len * kMaxTop * sizeof(unsigned long long));
         alloc((void**)&ctx->score_rows, (size_t)max_dims->total_nodes * sizeof(float2));
+        ctx->score_maxima_len = score_table_room(max_dims->total_nodes, max_dims->vocab);
+        alloc((void**)&ctx->score_maxima, (size_t)ctx->score_maxima_len * sizeof(float));
     }
     if (ok) {
         ok = cudaMemset(ctx->status, 0, sizeof(int32_t)) == cudaSuccess;
@@ -378,8 +379,8 @@ int owl_destroy(owl_ctx* ctx) {
     cudaFree(ctx->part_keys);
     cudaFree(ctx->lm_keys);
     cudaFree(ctx->score_part);
-    cudaFree(ctx->score_keys);
     cudaFree(ctx->score_rows);
+    cudaFree(ctx->score_maxima);
     for (auto& s : ctx->stg) cudaFree(s.p);
     for (auto& ev : ctx->ev)
         if (ev) cudaEventDestroy(ev);
@@ -803,7 +804,7 @@ int owl_token_logprobs(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const voi
     if (!logprob && !entropy && !lse && top == 0) return OWL_ERR_INVALID_ARG;
     if (dtype != OWL_DTYPE_BF16 && dtype != OWL_DTYPE_F16 && dtype != OWL_DTYPE_F32) return OWL_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(logits) % (dtype == OWL_DTYPE_F32 ? 4 : 2)) return OWL_ERR_INVALID_ARG;
-    if (top > kMaxTop) return OWL_ERR_UNSUPPORTED;
+    if (top > kMaxTop || d->vocab > 1 << 30) return OWL_ERR_UNSUPPORTED;
     if (!node_offsets && d->total_nodes % d->batch != 0) return OWL_ERR_INVALID_ARG;
     const long long most = ctx->score_len;
     if (!ctx->score_part || d->total_nodes > ctx->max_dims.total_nodes || ((long long)d->vocab + kScoreMaxChunk - 1) / kScoreMaxChunk > most)
@@ -812,12 +813,18 @@ int owl_token_logprobs(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const voi
     ScoreParams p{};
     p.logits = logits; p.tokens = tokens; p.node_offsets = node_offsets; p.tree_parent = tree_parent;
     p.logprob = logprob; p.entropy = entropy; p.lse = lse; p.top_ids = top_ids; p.top_logprobs = top_logprobs;
-    p.part = ctx->score_part; p.part_keys = ctx->score_keys; p.status = ctx->status;
+    p.part = ctx->score_part; p.maxima = ctx->score_maxima; p.status = ctx->status;
     p.batch = d->batch; p.total_nodes = d->total_nodes; p.nodes_uniform = d->total_nodes / d->batch; p.max_nodes = d->max_nodes;
     p.vocab = d->vocab; p.top = top;
     p.chunk = score_chunk(d->total_nodes, d->vocab, ctx->sm_count, most);
     p.chunks = (int32_t)(((long long)d->vocab + p.chunk - 1) / p.chunk);
-    const long long rows_at_once = most / p.chunks;
+    p.rounds = p.chunk / kScoreRound;
+    long long rows_at_once = most / p.chunks;
+    if (top > 0) {
+        const long long by_table = ctx->score_maxima_len / score_table(d->vocab, p.chunk);
+        if (by_table < 1) return OWL_ERR_TOO_LARGE;
+        if (by_table < rows_at_once) rows_at_once = by_table;
+    }
     if (d->total_nodes > rows_at_once) p.row_sums = ctx->score_rows;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     for (long long row0 = 0; row0 < d->total_nodes; row0 += rows_at_once) {

@@ -159,6 +159,38 @@ def test_many_rows_in_turns():
     c.close()
 
 
+@pytest.mark.parametrize("N,turns", [(20000, 1), (40000, 2)])
+def test_alternatives_of_many_rows_in_turns(N, turns):
+    """More groups of logits than the context's table has room for: a row of 3000 is one chunk of three rounds of 1024 and the ragged ones, 4 x 32
+    places; 20000 rows need 2.56 million of the 4.19 million places, 40000 rows 5.12 million."""
+    V = 3000
+    c = OwlContext(make_dims(batch=N // 50, total_nodes=N, max_nodes=50, vocab=V))
+    x = (4 * torch.randn((N, V), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)).half()
+    d = make_dims(batch=N // 50, total_nodes=N, max_nodes=50, vocab=V)
+    ids, best = torch.zeros((N, 6), dtype=torch.int32, device=DEV), torch.zeros((N, 6), device=DEV)
+    n0 = c.launch_count()
+    c.owl_token_logprobs(d, x, None, None, None, None, None, None, ids, best)
+    assert c.owl_get_status() == 0 and c.launch_count() - n0 == 2 * turns
+    v, i = torch.sort(x.float(), dim=1, descending=True, stable=True)
+    assert torch.equal(ids.long(), i[:, :6])
+    want = v[:, :6].double() - torch.logsumexp(x.double(), 1, keepdim=True)
+    assert float((best - want).abs().max()) <= REL + 8 * F32 * 40
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("tied", [20, 300, 1500, 30000])
+def test_ties_at_the_last_place(ctx, dtype, tied):
+    """Few larger logits and many that share the last alternative's value: up to more than the merge holds at once."""
+    rng = np.random.default_rng(tied)
+    x = rng.uniform(-3, 0, (3, 40003)).astype(np.float32)
+    for r in range(3):
+        at = rng.permutation(40003)
+        x[r, at[:tied]] = 2.0
+        x[r, at[tied:tied + 7]] = 2.0 + np.arange(1, 8)
+    check(ctx, x, rng.integers(0, 40003, 3), np.arange(4), None, 20, dtype)
+
+
 def test_malformed_trees_are_reported(ctx):
     rng = np.random.default_rng(7)
     x = torch.from_numpy(rng.standard_normal((9, 200)).astype(np.float32)).to(DEV)

@@ -107,6 +107,8 @@ int main() {
         if (what == 'e') { uint32_t u = (uint32_t)a; printf("%d\n", owl::block_exponent(u)); }
         if (what == 'c') printf("%d\n", owl::score_chunk(a, (int)b, (int)c, d));
         if (what == 'r') printf("%lld\n", owl::score_room(a, (int)b, (int)c));
+        if (what == 't') printf("%lld\n", owl::score_table((int)a, (int)b));
+        if (what == 'm') printf("%lld\n", owl::score_table_room(a, (int)b));
         if (what == 'h') printf("%d\n", owl::append_heads_per_group(a, (int)b, (int)c, (int)d));
     }
 }
@@ -145,7 +147,11 @@ def test_items_of_the_scan_fit_the_context(host):
     for (n, v), r, c in zip(calls, room, chunk):
         assert c % 1024 == 0 and 1024 <= c <= 16384 and r >= 2 * 148 * 16
         per_row = -(-v // c)
-        assert per_row <= r and (per_row * n <= r or c == 16384)
+        assert per_row <= r and (per_row * n <= r or per_row == 1 or c == 16384)
+    table = host([("t", v, c, 0, 0) for (n, v), c in zip(calls, chunk)])
+    table_room = host([("m", n, v, 0, 0) for n, v in calls])
+    for (n, v), c, t, m in zip(calls, chunk, table, table_room):
+        assert t == -(-v // c) * (c // 1024 + 1) * 32 and t <= m < 2 ** 31
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
