@@ -13,6 +13,7 @@
 
 #include "accept.cuh"
 #include "owl_common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace owl {
 
@@ -117,12 +118,28 @@ __device__ __forceinline__ void score_sums(ScoreState& st, const float (&x)[kCou
     }
     const float m = st.m;
     float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+    if constexpr (kCount == 1) {
+        const float d = fmaxf(x[0] - m, -200.f);
+        s0 = exp_of(d);
+        t0 = s0 * d;
+    } else {
+        // pairs, in packed arithmetic
+        using namespace sm100;
+        uint64_t s2 = 0ull, t2 = 0ull;
+        const uint64_t neg_m = pack_f32x2(-m, -m), log2e = pack_f32x2(1.4426950408889634f, 1.4426950408889634f);
 #pragma unroll
-    for (int i = 0; i < kCount; ++i) {
-        // -inf, a NaN, and the NaN of inf - inf all become a difference whose weight is 0
-        const float d = fmaxf(x[i] - m, -200.f), e = exp_of(d);
-        if (i & 1) { s1 += e; t1 = fmaf(e, d, t1); }
-        else { s0 += e; t0 = fmaf(e, d, t0); }
+        for (int i = 0; i < kCount; i += 2) {
+            // -inf, a NaN, and the NaN of inf - inf all become a difference whose weight is 0
+            float d0, d1, y0, y1;
+            unpack_f32x2(add_f32x2(pack_f32x2(x[i], x[i + 1]), neg_m), d0, d1);
+            const uint64_t d = pack_f32x2(fmaxf(d0, -200.f), fmaxf(d1, -200.f));
+            unpack_f32x2(mul_f32x2(d, log2e), y0, y1);
+            const uint64_t e = pack_f32x2(fast_exp2(y0), fast_exp2(y1));
+            s2 = add_f32x2(s2, e);
+            t2 = fma_f32x2(e, d, t2);
+        }
+        unpack_f32x2(s2, s0, s1);
+        unpack_f32x2(t2, t0, t1);
     }
     st.s += s0 + s1;
     st.t += t0 + t1;
