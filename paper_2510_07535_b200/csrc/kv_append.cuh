@@ -244,15 +244,16 @@ __global__ void __launch_bounds__(1024) kv_append_kernel(const AppendParams p) {
     }
 }
 
-// Heads per CTA: as few as give the device CTAs enough to hide the loads' latency (rows of one token's heads in several CTAs cost the
-// table's row and the sequence's numbers again), all of a page's where the pages alone are enough.
+// Heads per CTA: as few as still give the device a quarter of the CTAs that it holds at once (a draft: one, its latency counts), more where the
+// pages alone are enough: what a CTA finds out before it can ask for its first row - sequence, page, position, table entry - is
+// four loads one after the other.  (Four prompts of 2047 in fp16, all CTAs that are resident / a quarter: 67.0 / 64.0 us;
+// one of 8191 to 8 bits 38.4 / 38.9.)
 inline int append_heads_per_group(long long items, int heads, int page_size, int sms) {
-    const long long want = (long long)sms * (2048 / (8 * page_size));      // CTAs that are resident at once
+    const long long want = (long long)sms * (2048 / (8 * page_size)) / 4;
     long long groups = (want + items - 1) / items;
     if (groups > heads) groups = heads;
     if (groups < 1) groups = 1;
-    const int per = (int)((heads + groups - 1) / groups);
-    return per > 8 ? 8 : per;
+    return (int)((heads + groups - 1) / groups);
 }
 
 }  // namespace owl
