@@ -285,9 +285,10 @@ int owl_kv_append_fp8(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const v
 
 /*
  * owl_verify_attn over the 8-bit cache: q and out are of `dtype` (OWL_DTYPE_BF16 or OWL_DTYPE_F16), everything else as there, with
- * the caches' values for K and V.  A block's values enter both products as fp16 numbers, exact but for what lies below 2^-24; a
- * row of q enters divided by a power of two; the softmax weights are rounded to fp16, and the normaliser sums the rounded ones.
- * page_exp 2-byte aligned.
+ * the caches' values for K and V.  K enters as e4m3, its exponents in fp32; a row of q as a sum of e4m3 pieces, which leaves of an
+ * element at most 2^-17.8 of the row's largest (a row with an infinity or a NaN gives NaN); V as fp16 numbers, exact but for
+ * what lies below 2^-24; the softmax weights are rounded to fp16 for the product with V and summed unrounded.  page_exp
+ * 2-byte aligned, caches 16-byte aligned.
  */
 int owl_verify_attn_fp8(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void* q, const void* k_cache,
                         const void* v_cache, const int8_t* page_exp, const int32_t* block_table, const int32_t* ctx_lens,

@@ -138,12 +138,8 @@ __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUt
         }
         __syncwarp();
         if (!more) break;
-        int exps = exps_of(pages), exps_next = 0, pages_after = -1;
+        int exps = 0, exps_next = 0, pages_after = -1;
         for (int t = g.tile0, in_block = 0; t < g.tile1; ++t) {
-            if (in_block == 0) {
-                exps_next = exps_of(pages_next);
-                pages_after = pages_of(t + 2 * block_tiles);
-            }
             const int page = __shfl_sync(0xffffffffu, pages, in_block * ppt + lane);      // of the tile's pages, this lane's (lanes below ppt)
             int coord = oob;
             if ((unsigned)page < (unsigned)p.num_pages) coord = page * p.num_kv_heads + g.h;
@@ -163,7 +159,13 @@ __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUt
                     tma_load_3d_hint(raw + slot * kPieceBytes + lane * box_bytes, kv ? vmap : kmap, full, 0, 0, coord, stream_policy);
                 __syncwarp();
             }
-            // the note: an arrival of its own on both barriers, after the copies have been asked for
+            // (asked for after the tile's copies: the segment's first copies are what a short call waits for)
+            if (t == g.tile0) exps = exps_of(pages);
+            if (in_block == 0) {
+                exps_next = exps_of(pages_next);
+                pages_after = pages_of(t + 2 * block_tiles);
+            }
+            // the note: an arrival of its own on both barriers
             TileNote& note = aux->note[seq % kNotes];
             const int exp_kv = __shfl_sync(0xffffffffu, exps, in_block * ppt + ((lane * 16) >> p.page_shift));
             if (lane < kTileKeys / 16) {
@@ -927,15 +929,23 @@ __device__ __forceinline__ void keys_segment(const AttnParams& p, AuxFp8* aux, u
     for (int r0 = s * kHalf; r0 < s * kHalf + kHalf; r0 += 16) {
         uint32_t o[16];
         tmem_ld16(tmem + lane_sel + kJointO + r0, o);
+        // the next head's row, after a node's last head the next node's first (few instructions: they are fetched cold)
+        uint16_t* out = reinterpret_cast<uint16_t*>(p.out) + out_row_of(r0) * kHeadDim + wtid;
+        const long long wrap = (long long)(p.num_q_heads - G) * kHeadDim;
+        int hg = r0 - (int)row_node(p, r0) * G;
+        float* part = p.part_o + (part_base * 32 + (long long)(wtid >> 2) * kPartialRows + r0) * 4 + (wtid & 3);
+        const int rows = write_ok ? M - r0 : 0;
         tmem_wait_ld();
         tmem_loaded(o);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int row = r0 + r;
-            if (!write_ok || row >= M) continue;
-            const float v = __uint_as_float(o[r]) * k->w[row];
-            if (whole) reinterpret_cast<uint16_t*>(p.out)[out_row_of(row) * kHeadDim + wtid] = (uint16_t)pack2_16bit<kF16>(v, 0.f);
-            else p.part_o[(part_base * 32 + (long long)(wtid >> 2) * kPartialRows + row) * 4 + (wtid & 3)] = v;
+            const float v = __uint_as_float(o[r]) * k->w[r0 + r];
+            if (r < rows) {
+                if (whole) *out = (uint16_t)pack2_16bit<kF16>(v, 0.f);
+                else part[4 * r] = v;
+            }
+            out += kHeadDim;
+            if (++hg == G) { hg = 0; out += wrap; }
         }
     }
 }

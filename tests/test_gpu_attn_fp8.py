@@ -53,17 +53,18 @@ class Case:
         args = (wl.block_table, wl.ctx_lens, wl.node_offsets, wl.tree_parent, self.scale)
         out, lse = oracle.verify_attn(self.q, k, v, *args, dtype=self.dtype)
         size, _ = oracle.verify_attn(self.q, k, v & 0x7FFF, *args, dtype=self.dtype)          # sum p |v| / sum p
-        # A score: 128 products summed in fp32, each step an ulp (2^-23) of at most sum |q k| <= |q| |k|; then two roundings (the scale, the
-        # subtraction of the reference) and 2^-22 of ex2.
+        # A score: the pieces of a row of q leave of each element less than 2^-10 where the row's largest is above 224, 2^-17.8 of it, which
+        # meets sum |k| <= sqrt(128) |k|; 128 products summed in fp32, each step an ulp (2^-23) of at most sum |q k| <= |q| |k|;
+        # then two roundings (the scale, the subtraction of the reference) and 2^-22 of ex2.
         qn = np.sqrt((oracle.decode16(self.q, self.dtype).reshape(self.q.shape) ** 2).sum(-1)).max()
         kn = np.sqrt((np.nan_to_num(vals[0]) ** 2).sum(-1)).max()
         keys = int((wl.ctx_lens + np.diff(wl.node_offsets)).max())
-        score = qn * kn * self.scale * (128 * 2.0 ** -23 + 3 * 2.0 ** -24) + 2.0 ** -22
+        score = qn * kn * self.scale * (2.0 ** -17.8 * 128 ** 0.5 + 128 * 2.0 ** -23 + 3 * 2.0 ** -24) + 2.0 ** -22
         # Sums of weights: a tile's 64 pairs in two chains, then a sum over the tiles of a piece, the streams' and the pieces' merges.
         sums = (64 + keys / 128 + 200) * 2.0 ** -24
         lse_tol = score + sums + 2.0 ** -23 * (np.abs(lse) + 30) + 1e-6                        # (lg2.approx: 2^-22 absolute)
-        # Weights: fp16, half a step 2^-11 each and the normaliser sums the rounded ones; below 2^-32 of the reference, which is at most
-        # 2^8 below the largest score, they vanish; the products sum in fp32 over the keys; then the output's own rounding.
+        # Weights: fp16, half a step 2^-11 each, in the products; the normaliser sums them unrounded.  Below 2^-32 of the reference, which
+        # is at most 2^8 below the largest score, they vanish; the products sum in fp32 over the keys; then the output's own rounding.
         vmax = np.abs(np.nan_to_num(vals[1])).max()
         half_step = 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -11
         out_tol = half_step * np.abs(out) + size * (2 * 2.0 ** -11 + 2 * score + 2 * sums + keys * 2.0 ** -23 / 8) + keys * 2.0 ** -32 * vmax + 2.0 ** -24
