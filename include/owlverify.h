@@ -252,7 +252,8 @@ int owl_kv_commit(owl_ctx* ctx, const owl_dims* dims, void* k_cache, void* v_cac
  * dtype: OWL_DTYPE_BF16 or OWL_DTYPE_F16, that of q, k, v, q_out and the caches.  k, v [total_nodes, Hkv, 128], q [total_nodes,
  * Hq, 128]; a token's heads are contiguous, from one token to the next it is *_stride elements (a multiple of 8), so the three
  * may be parts of one projection's output.  q may be NULL (then num_q_heads and q_out are not looked at); q_out [total_nodes,
- * Hq, 128] contiguous receives the turned queries, and may be q itself where that is contiguous.  positions int32
+ * Hq, 128] contiguous receives the turned queries, and may be q itself where that is contiguous (any other overlap with q, k or v is
+ * OWL_ERR_INVALID_ARG).  positions int32
  * [total_nodes], NULL for ctx_lens[b] + i (a chain, a prompt); rope fp32 [rope_rows, 128], row m the 64 cosines and 64 sines of
  * position m (scaled as the model wants them); NULL, with rope_rows 0: nothing is turned.  block_table, ctx_lens, node_offsets
  * as for owl_verify_attn, but dims->total_nodes counts tokens of any number per sequence, none included (a prompt's too:
@@ -276,7 +277,8 @@ int owl_kv_append(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void*
  *
  * owl_kv_append_fp8 is owl_kv_append into such a cache (dtype is that of q, k, v and q_out).  A page whose first slot receives a
  * token takes the exponent that its new rows need; another page the larger of its own and that, and if it grows the rows of the
- * context on the page (those before ctx_lens[b]) are re-encoded.  A page that receives tokens must belong to one sequence only.
+ * context on the page (those before ctx_lens[b]) are re-encoded.  A page that receives tokens must belong to one sequence only and
+ * stand in its row of the block_table once.
  */
 int owl_kv_append_fp8(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void* q, int64_t q_stride, const void* k,
                       int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions, const float* rope,
@@ -286,7 +288,8 @@ int owl_kv_append_fp8(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const v
 /*
  * owl_verify_attn over the 8-bit cache: q and out are of `dtype` (OWL_DTYPE_BF16 or OWL_DTYPE_F16), everything else as there, with
  * the caches' values for K and V.  K enters as e4m3, its exponents in fp32; a row of q as a sum of e4m3 pieces, which leaves of an
- * element at most 2^-17.8 of the row's largest (a row with an infinity or a NaN gives NaN); V as fp16 numbers, exact but for
+ * element at most 2^-17.8 of the row's largest, or 2^-120 (a row with an infinity or a NaN gives NaN); a NaN in K or V reaches the
+ * rows that see its position and no others; V as fp16 numbers, exact but for
  * what lies below 2^-24; the softmax weights are rounded to fp16 for the product with V and summed unrounded.  page_exp
  * 2-byte aligned, caches 16-byte aligned.
  */

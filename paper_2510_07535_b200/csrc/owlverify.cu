@@ -747,6 +747,17 @@ static int kv_append_impl(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const 
     if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(rope) || !aligned16(q) || !aligned16(q_out) ||
         k_stride < 0 || v_stride < 0 || q_stride < 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || q_stride % 8 != 0)
         return OWL_ERR_INVALID_ARG;
+    if (q) {
+        // q_out may be q itself, row for row; anything else of q, k or v under it would be read after it has been written
+        const uintptr_t out = reinterpret_cast<uintptr_t>(q_out), out_end = out + (uintptr_t)d->total_nodes * d->num_q_heads * (kHeadDim * 2);
+        auto meets = [&](const void* x, int64_t stride, int heads) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(x), row = (uintptr_t)heads * (kHeadDim * 2);
+            return at < out_end && out < at + (uintptr_t)(d->total_nodes - 1) * (uintptr_t)stride * 2 + row;
+        };
+        const bool in_place = q == q_out && (d->total_nodes == 1 || q_stride == (int64_t)d->num_q_heads * kHeadDim);
+        if ((!in_place && meets(q, q_stride, d->num_q_heads)) || meets(k, k_stride, d->num_kv_heads) || meets(v, v_stride, d->num_kv_heads))
+            return OWL_ERR_INVALID_ARG;
+    }
     DeviceGuard guard(ctx->device);
     AppendParams p{};
     p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v);

@@ -298,3 +298,54 @@ def test_append_captured_and_replayed_on_another_stream(ctx):
     for got, want in zip(cache, (k8, v8, exp)):
         assert np.array_equal(got.view(torch.uint8 if want.dtype == np.uint8 else torch.int8).cpu().numpy(), want)
     del graph
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_queries_turned_in_place_and_overlaps_refused(ctx, fp8):
+    c = Case(10, "bf16", 4, 2, 16, [9, 30], [4, 7], fp8)
+    q, want, cache = c.parts(c.qkv.to(DEV))[0].contiguous(), c.expected(), c.on_device()
+    n0 = ctx.launch_count()
+    room = torch.zeros(2 * c.N * (4 + 2 + 2) * 128, dtype=torch.bfloat16, device=DEV)
+    fused = room[:c.N * 8 * 128].view(c.N, 8, 128)
+    fused.copy_(c.qkv)
+    fq, fk, fv = c.parts(fused)
+    contiguous = lambda at: room[at:at + c.N * 4 * 128].view(c.N, 4, 128)  # noqa: E731
+    for q_out in (contiguous(0), contiguous(128 * 8), contiguous((c.N * 8 - 2) * 128)):      # over q, over q from its second row on, over the last v
+        assert c.call(ctx, cache, fq, fk, fv, q_out, check=False) == -1
+    assert c.call(ctx, cache, fq, q[:, :2].contiguous(), fv, None, check=False) == -1
+    assert ctx.launch_count() == n0
+    c.call(ctx, cache, q, fk, fv, q)
+    assert ctx.owl_get_status() == 0
+    for got, w in zip((q, *cache), want):
+        assert same_bits(got.view(w.dtype), w)
+    # the place right behind the fused rows is free
+    assert c.call(ctx, cache, fq, fk, fv, contiguous(c.N * 8 * 128), check=False) == 0
+    assert same_bits(contiguous(c.N * 8 * 128), want[0]) and ctx.owl_get_status() == 0
+
+
+def test_a_long_prompt(ctx):
+    """140001 tokens of one sequence behind 77 others: 16 bits as they are, 8 bits by the format's formulas."""
+    L, n, hkv, page = 77, 140001, 2, 128
+    pages = -(-(L + n) // page)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    kv = torch.randn(n, 2 * hkv, 128, generator=g, device=DEV).bfloat16()
+    k, v = kv[:, :hkv], kv[:, hkv:]
+    table = torch.randperm(pages, generator=g, device=DEV).int().view(1, -1)
+    d = make_dims(batch=1, total_nodes=n, max_nodes=1, num_q_heads=1, num_kv_heads=hkv, page_size=page, max_pages_per_seq=pages, num_pages=pages)
+    rows = lambda cache: cache[table[0].long()].transpose(1, 2).reshape(pages * page, hkv, 128)  # noqa: E731
+    caches = [torch.zeros(pages, hkv, page, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    ctx.owl_kv_append(d, None, k, v, None, None, None, *caches, table, dev_i32([L]), None)
+    for cache, x in zip(caches, (k, v)):
+        assert torch.equal(rows(cache)[L:L + n], x) and not rows(cache)[:L].any() and not rows(cache)[L + n:].any()
+    c8 = [torch.zeros(pages, hkv, page, 128, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn) for _ in range(2)]
+    exp = torch.full((pages, hkv, 2), -24, dtype=torch.int8, device=DEV)
+    ctx.owl_kv_append_fp8(d, None, k, v, None, None, None, *c8, exp, table, dev_i32([L]), None)
+    for i, (cache, x) in enumerate(zip(c8, (k, v))):
+        full = torch.zeros(pages * page, hkv, 128, device=DEV, dtype=torch.float64)
+        full[L:L + n] = x.double()
+        blocks = full.view(pages, page, hkv, 128)
+        e = torch.ceil(torch.log2(blocks.abs().amax((1, 3)) / 448))            # [pages, hkv]; no magnitude here is 448 times a power of two by a hair
+        assert torch.equal(exp[table[0].long()][..., i].double(), e)
+        want = (blocks * torch.exp2(-e)[:, None, :, None]).float().to(torch.float8_e4m3fn).view(pages * page, hkv, 128)
+        assert torch.equal(rows(cache.view(torch.uint8)), want.view(torch.uint8))
+    assert ctx.owl_get_status() == 0

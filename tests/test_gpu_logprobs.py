@@ -231,3 +231,32 @@ def test_refusals(ctx):
     attn_only = OwlContext(make_dims(batch=1, total_nodes=4, max_nodes=4))
     assert attn_only.owl_token_logprobs(d, x, tok, None, None, f, check=False) == -7
     attn_only.close()
+
+
+def test_more_than_2_to_the_31_logits():
+    """The last rows of an array of 2^31 elements and more, among them a chain whose parents lie on both sides of that."""
+    N, V = 16800, 128256
+    x = torch.empty(N, V, dtype=torch.float16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    for r in range(0, N, 64):
+        x[r:r + 64] = torch.randn(min(64, N - r), V, generator=g, device=DEV)
+    c = OwlContext(make_dims(batch=N // 60, total_nodes=N, max_nodes=60, vocab=V))
+    d = make_dims(batch=N // 60, total_nodes=N, max_nodes=60, vocab=V)
+    tok = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    par = torch.arange(-1, 59, dtype=torch.int32, device=DEV).repeat(N // 60)
+    lp, ent, lse, ids, best = (torch.zeros(N, device=DEV), torch.zeros(N, device=DEV), torch.zeros(N, device=DEV),
+                               torch.zeros(N, 3, dtype=torch.int32, device=DEV), torch.zeros(N, 3, device=DEV))
+    c.owl_token_logprobs(d, x, tok, None, par, lp, ent, lse, ids, best)
+    assert c.owl_get_status() == 0
+    rows = [0, 1, 16743, 16744, 16745, N - 2, N - 1]                # 2^31 / V = 16743.8
+    y = x[rows].double().cpu().numpy()
+    _, r_ent, r_lse, r_ids, r_best = oracle.token_logprobs(y, np.zeros(len(rows), np.int32), np.array([0, len(rows)], np.int32), None, 3)
+    np.testing.assert_array_equal(ids[rows].cpu().numpy(), r_ids)
+    tol = tolerance(y, r_lse)
+    assert (np.abs(lse[rows].double().cpu().numpy() - r_lse) <= tol).all() and (np.abs(best[rows].double().cpu().numpy() - r_best) <= tol[:, None]).all()
+    assert np.abs(ent[rows].double().cpu().numpy() - r_ent).max() <= 4 * REL * (np.log(V) + 1) + 8 * F32 * (np.log(V) + 1)
+    p = par.cpu().numpy()
+    for n in (16743, 16744, 16745, 16746, N - 1):
+        want = 0.0 if p[n] < 0 else float(x[n - n % 60 + p[n], tok[n].item()]) - float(torch.logsumexp(x[n - n % 60 + p[n]].double(), 0))
+        assert abs(float(lp[n]) - want) <= tol.max()
+    c.close()
