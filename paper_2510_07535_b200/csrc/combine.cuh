@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kCombineThreads, kCombineCtasPerSm) combine_sc
             mx_new = fmaxf(mx_new, __shfl_xor_sync(0xffffffffu, mx_new, 16));
             float round_sum = 0.f;
             for (int j = lane >> 3; j < cnt; j += 4) {
-                const float l = lse_stage[j * 8 + r], w = l > -INFINITY ? __expf(l - mx_new) : 0.f;     // an empty partial has no weight
+                const float l = lse_stage[j * 8 + r], w = l == -INFINITY ? 0.f : __expf(l - mx_new);    // an empty partial has no weight; a NaN's is one
                 lse_stage[j * 8 + r] = w;
                 round_sum += w;
             }
@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(kCombineThreads, kCombineCtasPerSm) combine_sc
             pk.x = *reinterpret_cast<uint32_t*>(&lo2);
             pk.y = *reinterpret_cast<uint32_t*>(&hi2);
         }
-        const float lse = sum > 0.f ? mx + logf(sum) : -INFINITY;
+        const float lse = sum > 0.f ? mx + logf(sum) : sum == 0.f ? -INFINITY : sum;
         // rows past the unit's last hold nothing; a bad tree or page in the unit's sequence (the same for all of its rows): no
         // output
         if (!__any_sync(0xffffffffu, bad) && out_row >= 0) {

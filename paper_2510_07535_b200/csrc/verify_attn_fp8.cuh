@@ -12,7 +12,10 @@
 //
 // Two e4m3 products of 128x128x32 take the time of one fp16 pair, so the tensor pipe does the work of the 16-bit caches' pass; HBM brings half
 // of its bytes, and shared memory carries per tile 32 KB from TMA, 64 for Q K^T, 16 + 32 for the conversion and 32 for P V.  (A
-// form that turned K into fp16 as well moved 224 KB, kept the ring half as deep, and took 453 instead of %CH% us on 16 chains of 8 at 4K to 64K.)
+// form that turned K into fp16 as well moved 224 KB, kept the ring half as deep, and took 453 instead of 283 us on 16 chains of 8 at 4K to 64K.)
+// What bounds it: from some 16 long sequences on the board's 1000 W.  16 chains run at 1.9 GHz and 4.0 TB/s, 62 % of the copy
+// bandwidth; 16 trees of 32, 128 rows a unit, at 1.6 GHz and 850 TFLOP/s of Q K^T and P V (and weights of 16 ex2 a clock: 1024
+// of a tile's 1700 clocks); one tree of 32 at 32K (31 us) and a chain at 2K (13 us) are set-up, first copies and the merge.
 //
 // 16 warps:
 //   warp 0        TMA producer: one box per (page, head) of K and of V into a ring of tiles of 2 x 16 KB; leaves each tile's note
@@ -24,7 +27,7 @@
 // verify_attn_umma.cuh.
 // Other units ("joint"): both softmax warpgroups work on each tile, one O, and three S, so that Q K^T runs up to three tiles ahead and no
 // softmax waits for the products of the tile before.  (With two streams that took the tiles by turns, each waiting for its own
-// P V and Q K^T, a 128-row tile took 2100 clocks: %J1%.)
+// P V and Q K^T, a 128-row tile took 2100 clocks: 16 chains of 64-row units 411 us instead of 312.)
 //   65 to 128 rows: rows on the lanes, each warpgroup weighs half of a tile's keys; the two share the rows' references.
 //   up to 64 rows:  keys on the lanes.  The products are turned round,
 //       S^T = K Q^T   [128 keys x pieces * rows], the pieces' columns added up in registers,
@@ -79,7 +82,7 @@ __device__ __forceinline__ uint32_t joint_s(uint32_t buffer, uint32_t columns) {
 // Q K^T, and that at most three tiles ahead of the softmax warps, the last to look at it.
 struct TileNote {
     float kscale[kTileKeys / 16];                // 2^e of K, for each 16 keys
-    int valid;                                   // keys of the sequence in it; -1: no more tiles
+    int spans;                                   // low half: keys of the sequence in it (-1: no more tiles); high: of them, the context's
     int8_t vexp[kTileKeys / 16];                 // e of V
 };
 struct AuxFp8 : Aux {
@@ -87,6 +90,7 @@ struct AuxFp8 : Aux {
     uint64_t v_full[kFp8VSlots], v_empty[kFp8VSlots];
     uint64_t joint_s_full[3], joint_o_done;
     TileNote note[kNotes];
+    uint8_t nan_drafts[kNotes];                  // of the tile: a drafted row of V has a NaN, which its fp16 tile has not
     float row_scale[kRows];                      // what the rows of Q were divided by
 };
 static_assert(sizeof(AuxFp8) <= kAuxBytes, "aux area too small");
@@ -172,7 +176,10 @@ __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUt
                 note.kscale[lane] = exp2_int(max(kExpMin, min(kExpMax, (int)(int8_t)(exp_kv & 0xff))));
                 note.vexp[lane] = (int8_t)(exp_kv >> 8);
             }
-            if (lane == 0) note.valid = min(kTileKeys, keys - t * kTileKeys);
+            if (lane == 0) {
+                note.spans = min(kTileKeys, keys - t * kTileKeys) | max(0, min(kTileKeys, g.L - t * kTileKeys)) << 16;
+                aux->nan_drafts[seq % kNotes] = 0;
+            }
             __syncwarp();
             if (lane < 2) mbar_arrive(smem_u32(&aux->raw_full[2u * place + lane]));
             if (++in_block == block_tiles) { in_block = 0; pages = pages_next; exps = exps_next; pages_next = pages_after; }
@@ -183,17 +190,41 @@ __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUt
     // no more tiles (after a wait that gave up the converting warps stop by themselves)
     const bool ok = mbar_wait(smem_u32(&aux->raw_empty[2u * place + 1u]), free_parity, abort_flag);
     if (lane == 0 && ok) {
-        aux->note[seq % kNotes].valid = -1;
+        aux->note[seq % kNotes].spans = -1;
         mbar_arrive(smem_u32(&aux->raw_full[2u * place + 1u]));
         mbar_arrive(smem_u32(&aux->raw_full[2u * place + 1u]));
     }
 }
 
 // ------------------------------------------------------------------------------------------ V to fp16
-// Warp w of four takes key groups 4w .. 4w + 3 of a tile, eight keys x 64 elements per turn.  Lane: 16 elements (one 16-byte piece) of
+// Warp w of four takes key groups 4w .. 4w + 3 of a tile, eight keys x 64 elements per turn `j`.  Lane: 16 elements (one 16-byte piece) of
 // one key.  Raw rows are 128 bytes with piece x at place x ^ (key & 7), operand rows 128 bytes per half of the head dimension with
 // piece y at y ^ (key & 7), and a raw piece becomes operand pieces 2x, 2x + 1: eight neighbouring lanes take four pieces of two keys
 // that differ in bits 0 and 2, so that neither the loads nor the stores meet in a bank.
+__device__ __forceinline__ uint4 load_v(const unsigned char* src, int j, int piece, int key7) {
+    return *reinterpret_cast<const uint4*>(src + (j >> 1) * 1024 + ((((j & 1) * 4 + piece) ^ key7) << 4));
+}
+__device__ __forceinline__ void convert_v(const uint4& u, int j, const TileNote& note, int warp, unsigned char* dst, int piece, int key7) {
+    const int e = max(kExpMin, min(kExpMax, (int)note.vexp[2 * warp + (j >> 2)]));
+    const uint32_t one = e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24);
+    const uint32_t two_to_e = one | one << 16;
+    uint32_t o[8];
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = e4m3x2_to_f16x2(w[i] & 0xffffu), b = e4m3x2_to_f16x2(w[i] >> 16);
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i]) : "r"(a), "r"(two_to_e));
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i + 1]) : "r"(b), "r"(two_to_e));
+    }
+    unsigned char* to = dst + (j >> 1) * 2048 + (j & 1) * 1024;
+    *reinterpret_cast<uint4*>(to + (((2 * piece) ^ key7) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<uint4*>(to + (((2 * piece + 1) ^ key7) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+}
+__device__ __forceinline__ uint32_t drop_nans(uint32_t& v) {
+    const uint32_t nans = __vcmpeq4(v & 0x7f7f7f7fu, 0x7f7f7f7fu);
+    v &= ~nans;
+    return nans;
+}
 template <bool kWide, bool kF16>
 __device__ __forceinline__ void convert_loop(const AttnParams& p, AuxFp8* aux, unsigned char* smem) {
     constexpr uint32_t kPlaces = kRawTiles<kWide, kF16>;
@@ -207,38 +238,32 @@ __device__ __forceinline__ void convert_loop(const AttnParams& p, AuxFp8* aux, u
     for (uint32_t n = 0;; ++n) {
         if (!__all_sync(kAll, mbar_wait(smem_u32(&aux->raw_full[2u * place + 1u]), parity, abort_flag))) return;
         const TileNote& note = aux->note[n % kNotes];
-        const int valid = const_cast<const volatile int&>(note.valid);
+        const int spans = const_cast<const volatile int&>(note.spans), valid = (int16_t)(spans & 0xffff), context = spans >> 16;
         if (valid < 0) return;
         const uint32_t slot = n % kFp8VSlots;
         if (!__all_sync(kAll, mbar_wait(smem_u32(&aux->v_empty[slot]), ((n / kFp8VSlots) & 1u) ^ 1u, abort_flag))) return;
         const unsigned char* src = raw + 2u * place * kPieceBytes;
         unsigned char* dst = ring + slot * kSlotBytes;
-        uint4 u[8];
+        if (__builtin_expect(context >= valid, 1)) {      // the context's keys alone, all of the tile
+            uint4 u[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            u[j] = *reinterpret_cast<const uint4*>(src + (j >> 1) * 1024 + ((((j & 1) * 4 + piece) ^ key7) << 4));
+            for (int j = 0; j < 8; ++j) u[j] = load_v(src, j, piece, key7);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int group = 4 * warp + (j >> 1);                     // of eight keys
-            const int e = max(kExpMin, min(kExpMax, (int)note.vexp[group >> 1]));
-            const uint32_t one = e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24);
-            const uint32_t two_to_e = one | one << 16;
-            uint32_t o[8];
-            const uint32_t w[4] = {u[j].x, u[j].y, u[j].z, u[j].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t a = e4m3x2_to_f16x2(w[i] & 0xffffu), b = e4m3x2_to_f16x2(w[i] >> 16);
-                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i]) : "r"(a), "r"(two_to_e));
-                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * i + 1]) : "r"(b), "r"(two_to_e));
+            for (int j = 0; j < 8; ++j) convert_v(u[j], j, note, warp, dst, piece, key7);
+        } else {
+            // A tile that holds drafted rows, or ends.  Rows past the sequence's end may hold anything, and their weight of 0 does not make a
+            // NaN harmless; nor does it that of a drafted row in the rows of Q that do not see its node: such NaNs are left out, and those that
+            // do see it get them at the segment's end (mark_nan_drafts).  Apart from the other tiles, and short: with this looked at in
+            // every tile 16 mixed sequences of 4K to 64K took 468 us, unrolled by two in the loop's middle 360, like this 340.
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                const int key = (4 * warp + (j >> 1)) * 8 + key7;
+                uint4 u = load_v(src, j, piece, key7);
+                if (key >= valid) u = make_uint4(0u, 0u, 0u, 0u);
+                else if (key >= context && (drop_nans(u.x) | drop_nans(u.y) | drop_nans(u.z) | drop_nans(u.w)))
+                    const_cast<volatile uint8_t&>(aux->nan_drafts[n % kNotes]) = 1;
+                convert_v(u, j, note, warp, dst, piece, key7);
             }
-            // rows past the sequence's end may hold anything, and their weight of 0 does not make a NaN harmless
-            if (group * 8 + key7 >= valid) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = 0u;
-            }
-            unsigned char* to = dst + (j >> 1) * 2048 + (j & 1) * 1024;
-            *reinterpret_cast<uint4*>(to + (((2 * piece) ^ key7) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<uint4*>(to + (((2 * piece + 1) ^ key7) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -434,8 +459,8 @@ __device__ __forceinline__ void load_q_fp8(const AttnParams& p, const Segment& g
             }
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-            // the smallest power of two with (largest magnitude) <= 448 of them (block_exponent, over fp32's range)
-            const int e = max(-110, min(110, (int)((most + 0x1fffffu) >> 23) - 135));
+            // the smallest power of two with (largest magnitude) <= 448 of them (block_exponent, over the types' range)
+            const int e = max(-110, min(120, (int)((most + 0x1fffffu) >> 23) - 135));
             const float inv = exp2_int(-e);
             float y[8];
 #pragma unroll
@@ -459,7 +484,7 @@ __device__ __forceinline__ void load_q_fp8(const AttnParams& p, const Segment& g
 
 // Weights are kept 2^7 above exp2(score - m), up to 2^15, so that fp16 (largest 65504, smallest step 2^-24) holds what is 2^-31 of the
 // reference.  The normaliser sums them as they are, not as fp16 rounds them: that is off by at most 2^-12 of the output, where one
-// key has all the weight, and two conversions and an addition per pair of keys less (70B with 32 nodes 647 -> 592 us).
+// key has all the weight, and two conversions and an addition per pair of keys less (8 trees of 32 at 64K, 64 query heads: 647 -> 592 us).
 constexpr float kWeightShift = 7.f;
 constexpr float kWeightLimit = 32768.f;          // 2^(8 + 7)
 // log-sum-exp of a row from its reference and its sum of shifted weights (a NaN sum stays one)
@@ -474,6 +499,13 @@ __device__ __forceinline__ float from_ordered(unsigned u) { return u == 0u ? -IN
 __device__ __forceinline__ float min_or_nan(float x, float y) {
     float r;
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+// What a row's sums of products are multiplied by, besides their page's 2^e.  Not below 2^-100, where all that is less makes scores that differ
+// by less than 2^-66: times 2^-24 it is no zero, and a score of -inf stays one.  (A NaN stays one, too.)
+__device__ __forceinline__ float score_scale(const AttnParams& p, float row_scale) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(p.sm_scale * 1.4426950408889634f * row_scale), "f"(exp2_int(-100)));
     return r;
 }
 // Meets `count` threads on hardware barrier `id`; true for all if it is for one.
@@ -517,7 +549,7 @@ __device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, u
     const int live = live_warps_fp8(g.M), both = 64 * live;      // threads of the two warpgroups that hold rows
     const bool idle = (wtid >> 5) >= live;
     const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
-    const float scale2 = p.sm_scale * 1.4426950408889634f * aux->row_scale[rr];
+    const float scale2 = score_scale(p, aux->row_scale[rr]);
     float m = -INFINITY, l = 0.f;          // the row's reference, alike in both warpgroups; the sum over this one's keys
     uint32_t b = 0, p_bar = 0;
     for (int i = 0; i < (idle ? 0 : T); ++i) {
@@ -694,7 +726,7 @@ struct KeysStream {
         if (wtid < kHalf) {
             const int row = row0() + wtid;
             // rows beyond M: weights of 0; others: any score at all is above the threshold until the first reference is there
-            k->scale[row] = row < g.M ? p.sm_scale * 1.4426950408889634f * aux->row_scale[row] : 0.f;
+            k->scale[row] = row < g.M ? score_scale(p, aux->row_scale[row]) : 0.f;
             k->bias[row] = row < g.M ? 1e30f : -INFINITY;
             k->m[row] = -INFINITY;
         }
@@ -1002,7 +1034,7 @@ __device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux,
     const uint32_t tS = tmem + lane_sel + s * 128, tO = tS + 256;
     const int rr = s * 128 + wtid, T = g.tile1 - g.tile0;
     const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
-    const float scale2 = p.sm_scale * 1.4426950408889634f * aux->row_scale[rr];
+    const float scale2 = score_scale(p, aux->row_scale[rr]);
     float m = -INFINITY, l = 0.f;
     for (int i = 0; i < T; ++i) {
         const int t = g.tile0 + i;
@@ -1158,6 +1190,31 @@ __device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux,
     }
 }
 
+// The segment's results are stored: those of rows that see a drafted node whose V has a NaN become one, channel by channel, from the
+// rows of V in the cache (convert_loop left the NaNs out; a thread per row of the unit).
+__device__ __forceinline__ void mark_nan_drafts(const AttnParams& p, AuxFp8* aux, uint32_t seg_no) {
+    const volatile Segment& g = aux->seg[seg_no % kSegs];
+    const int row = threadIdx.x - 128, L = g.L, G = p.group;
+    if (row >= g.M || const_cast<volatile int&>(aux->seg_bad_tree) || g.bad_page || *const_cast<volatile int*>(&aux->abort_flag)) return;
+    const int node = (int)row_node(p, row);
+    const long long out_row = (long long)(g.node_base + node) * p.num_q_heads + g.h * G + (row - node * G);
+    float* part = p.part_o + ((2ll * blockIdx.x + (seg_no > 0 ? 1 : 0)) * kPartialRows * 32 + row) * 4;      // [32 groups of four channels][rows][4]
+    const bool whole = g.tile0 == 0 && g.tile1 == g.tiles;
+#pragma unroll 1
+    for (unsigned long long seen = aux->anc[node]; seen; seen &= seen - 1ull) {
+        const int pos = L + __ffsll((long long)seen) - 1;
+        const int page = p.block_table[(long long)g.b * p.max_pages_per_seq + (pos >> p.page_shift)];
+        const uint8_t* v = reinterpret_cast<const uint8_t*>(p.v_cache) +
+                           (((long long)page * p.num_kv_heads + g.h) * p.page_size + (pos & (p.page_size - 1))) * kHeadDim;
+#pragma unroll 1
+        for (int c = 0; c < kHeadDim; ++c) {
+            if ((unsigned)page >= (unsigned)p.num_pages || (v[c] & 0x7f) != 0x7f) continue;
+            if (whole) reinterpret_cast<uint16_t*>(p.out)[out_row * kHeadDim + c] = 0x7fff;      // a NaN of either type
+            else part[(c >> 2) * (kPartialRows * 4) + (c & 3)] = __int_as_float(0x7fffffff);
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------ softmax warpgroups
 template <bool kWide, bool kF16>
 __device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* aux, unsigned char* smem, uint32_t tmem, const int s /*warpgroup*/) {
@@ -1217,7 +1274,14 @@ __device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* au
             ++joint_segs;
         }
         tc_fence_before();
-        tile_base += (uint32_t)(g.tile1 - g.tile0);
+        const uint32_t T = (uint32_t)(g.tile1 - g.tile0);
+        tile_base += T;
+        // (drafted rows lie in the last two tiles of a sequence at most; alike in all threads)
+        const volatile uint8_t* nans = aux->nan_drafts;
+        if (nans[(tile_base - 1u) % kNotes] || (T > 1u && nans[(tile_base - 2u) % kNotes])) {
+            named_barrier(1, 256);               // the results, which other threads have stored
+            mark_nan_drafts(p, aux, seg_no);
+        }
         ++seg_no;
     }
 }

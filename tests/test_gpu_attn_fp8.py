@@ -261,3 +261,63 @@ def test_refusals():
             run(ctx, {**t, name: bad})
     assert ctx.launch_count() == n0 and ctx.owl_get_status() == 0
     ctx.close()
+
+
+@pytest.mark.parametrize("hq,hkv,trees,ctx", [
+    (8, 2, [("tree", 8, 3)], [300]),                    # 32 rows
+    (8, 2, [("tree", 8, 3), ("tree", 16, 4)], [0, 120]),      # 64 rows, drafts over two tiles
+    (8, 2, [("tree", 31, 5)], [1000]),                  # 124 rows
+    (8, 2, [("tree", 60, 8)], [70]),                    # 240 rows, drafts over two tiles
+    (4, 2, [("tree", 30, 4), ("tree", 64, 8)], [9000, 40000]),      # segments of several CTAs
+])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_nan_of_a_drafted_node_reaches_the_rows_that_see_it(hq, hkv, trees, ctx, dtype):
+    """One node's V has a NaN in two channels of one KV head, another's K one; nodes beside them do not see either."""
+    c = Case(W.Spec("nandraft", hq, hkv, ctx, trees, shuffle_pages=True, seed=10), dtype)
+    out, lse, out_tol, lse_tol = c.reference()
+    wl, G = c.wl, hq // hkv
+    bad, bad_lse = np.zeros(out.shape, bool), np.zeros(lse.shape, bool)
+    for b, L in enumerate(wl.ctx_lens):
+        o, n = wl.node_offsets[b], wl.node_offsets[b + 1] - wl.node_offsets[b]
+        sees = np.zeros((n, n), bool)
+        for i in range(n):
+            p = wl.tree_parent[o + i]
+            sees[i] = sees[p] if p >= 0 else False
+            sees[i, i] = True
+        alone = [j for j in range(1, n) if 0 < sees[:, j].sum() < n - 1]
+        jv, jk = alone[0], alone[-1]
+        for j, cache, channels in ((jv, c.v8, (3, 97)), (jk, c.k8, (50,))):
+            pos = int(L) + j
+            cache[wl.block_table[b, pos // wl.k_cache.shape[2]], 1, pos % wl.k_cache.shape[2], list(channels)] = 0x7F if j == jv else 0xFF
+        rows = o + np.arange(n)
+        for ch in (3, 97):
+            bad[rows[sees[:, jv]], G:2 * G, ch] = True
+        bad[rows[sees[:, jk]], G:2 * G] = True
+        bad_lse[rows[sees[:, jk]], G:2 * G] = True
+    t = c.device()
+    ctx = OwlContext(c.dims())
+    run(ctx, t)
+    assert ctx.owl_get_status() == 0
+    got, got_lse = t["out"].double().cpu().numpy(), t["lse"].double().cpu().numpy()
+    np.testing.assert_array_equal(np.isnan(got), bad)
+    np.testing.assert_array_equal(np.isnan(got_lse), bad_lse)
+    assert (np.abs(got - out)[~bad] <= out_tol[~bad]).all() and (np.abs(got_lse - lse)[~bad_lse] <= lse_tol[~bad_lse]).all()
+    ctx.close()
+
+
+def test_queries_and_keys_of_nothing():
+    """Rows of zeros against pages of zeros at the smallest exponent and a tiny scale: what a row does not see stays out all the same."""
+    for trees, ctx in (([("tree", 8, 3)], [300]), ([("tree", 30, 5)], [90]), ([("tree", 60, 6)], [100])):
+        c = Case(W.Spec("zero8", 8, 2, ctx, trees, shuffle_pages=True, seed=12))
+        c.q[:], c.k8[:], c.exp[..., 0], c.scale = 0, 0, -24, 1e-20
+        check(c)
+
+
+def test_queries_at_the_end_of_their_range():
+    """Queries up to the largest bf16 numbers, brought back by small keys and the scale."""
+    for trees, ctx in (([("tree", 8, 3)], [300]), ([("tree", 30, 5)], [90]), ([("tree", 60, 6)], [100])):
+        c = Case(W.Spec("huge8", 8, 2, ctx, trees, shuffle_pages=True, seed=13))
+        q = W.bf16_bits_to_f32(c.wl.q).astype(np.float64)
+        c.q = bits16(q * (2.0 ** 127.5 / np.abs(q).max()), "bf16")
+        c.exp[..., 0], c.scale = -24, 2.0 ** -116
+        check(c)
