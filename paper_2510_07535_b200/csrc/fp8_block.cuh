@@ -2,8 +2,8 @@
 // for v * 2^e, with one whole exponent e per block.  A power of two, so that
 //   * a block whose exponent has to grow (a larger row is appended) is re-encoded by shifting: exact but for what drops below
 //     e4m3's smallest step, where any scale would have put it too;
-//   * the attention pass turns a block into fp16 without a rounding: e4m3's four significant bits times 2^e, -24 <= e <= 7,
-//     is an fp16 number unless it is below 2^-24 steps (e < -15 and a value in e4m3's own subnormal range).
+//   * the attention pass puts K's exponent into the fp32 scores, exactly, and turns V into fp16 without a rounding: e4m3's four
+//     significant bits times 2^e, -24 <= e <= 7, is an fp16 number but for what lies below fp16's smallest step, 2^-24.
 // e is the smallest exponent in [kExpMin, kExpMax] with (largest magnitude) <= 448 * 2^e; what exceeds 448 * 2^7 = 57344
 // (fp16's own range ends at 65504) saturates there.
 #pragma once

@@ -12,6 +12,10 @@
 // table entries stay in registers over all its heads, and a block's largest magnitude is a reduction over the CTA.  Items
 // (pages) are numbered without a prefix sum over the batch: sequence b's begin at floor(offset_b / page) + 2 b, because
 // n tokens touch at most floor(n / page) + 2 pages wherever they begin.
+//
+// Bound by the rows' bytes for a prompt, by one chain of dependent loads (offsets, length, table, row) for a draft: 8191 tokens to 8
+// bits with 32 + 16 heads take 38.5 us (189 MB, 4.9 TB/s, 75 % of the copy bandwidth), four prompts of 2047 in fp16 63.6 us (340 MB,
+// 5.3 TB/s, 81 %), a chain of 8 or 16 trees of 32 about 3 and 5 us on the device and 9.3 us from call to call, which is the host's.
 #pragma once
 
 #include "fp8_block.cuh"

@@ -29,6 +29,8 @@ __device__ __forceinline__ uint4 rescale_e4m3x16(const uint4& u, float f) {
     return make_uint4(rescale_e4m3x4(u.x, f), rescale_e4m3x4(u.y, f), rescale_e4m3x4(u.z, f), rescale_e4m3x4(u.w, f));
 }
 
+// Bound by latency, the exponents (a load behind the table's) and the rows: 3.4 us for one tree of 32, 4.5 for 64 trees, 9.5 us from
+// call to call.
 // grid and clusters as kv_commit_kernel: a sequence's heads are dealt out to its cluster's CTAs, half of a CTA's threads move K,
 // half V, eight threads (16 bytes each) to a row.
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_fp8_kernel(const CommitFp8Params fp) {

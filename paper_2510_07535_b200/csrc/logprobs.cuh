@@ -7,6 +7,8 @@
 //   logprob_merge_kernel  a CTA per row joins the chunks:  lse = m + ln s,  entropy = ln s - t / s,  scores a token, and finds
 //                         the alternatives: of 64 maxima over parts of the table the top-th largest is not above the top-th
 //                         largest logit, so the groups of 32 whose maximum reaches it hold all of them, some tens of groups.
+// 256 rows of 128256 fp32 logits with 20 alternatives take 30.2 us (131 MB, 4.3 TB/s, 66 % of the copy bandwidth); 8 rows 9.3 us, the
+// latency of two launches.
 // Bound by the logits' bytes: per element a maximum, a subtraction, a product, a clamp, an ex2 and two sums.  (A sorted list per warp in the
 // scan instead of the table: 256 rows of 128256 fp32 logits 42.8 us with 20 alternatives and 23.9 without, 8 rows 13.9 and 2.7.)
 #pragma once
