@@ -184,3 +184,54 @@ def test_two_contexts_on_two_streams():
     for s in sides:
         assert s[0].owl_get_status() == 0
         s[0].close()
+
+
+def test_a_captured_step_replayed():
+    """Append, attention, log probabilities and commit in one graph: each replay is the next step, lengths and cache only ever on the device."""
+    hq, hkv, page, n, rounds = 8, 2, 16, 6, 7
+    g = torch.Generator(device=DEV).manual_seed(6)
+    lens = [5000, 3, 700]
+    B, width = 3, 330
+    d = make_dims(batch=B, total_nodes=B * n, max_nodes=n, num_q_heads=hq, num_kv_heads=hkv, page_size=page, max_pages_per_seq=width,
+                  num_pages=B * width, sm_scale=0.05, vocab=5000)
+    kv = [torch.randint(0, 0x7F, (B * width, hkv, page, 128), generator=g, device=DEV, dtype=torch.uint8).view(torch.float8_e4m3fn) for _ in range(2)]
+    kv.append(torch.randint(-8, -4, (B * width, hkv, 2), generator=g, device=DEV, dtype=torch.int8))
+    qkv = torch.randn(B * n, hq + 2 * hkv, 128, generator=g, device=DEV).bfloat16()
+    rope = torch.randn(6000, 128, generator=g, device=DEV)
+    table = torch.randperm(B * width, generator=g, device=DEV).int().view(B, width)
+    par = dev_i32([-1, 0, 0, 1, 2, 3] * B)
+    alen, path = dev_i32([3, 4, 1]), torch.full((B, 64), -1, dtype=torch.int32, device=DEV)
+    path[0, :3], path[1, :4], path[2, :1] = dev_i32([0, 2, 4]), dev_i32([0, 1, 3, 5]), dev_i32([0])
+    logits, tok = torch.randn(B * n, 5000, generator=g, device=DEV), torch.randint(0, 5000, (B * n,), generator=g, device=DEV).int()
+    ctx = OwlContext(d)
+
+    class State:
+        def __init__(self):
+            self.cache, self.L = [x.clone() for x in kv], dev_i32(lens)
+            self.q, self.out = (torch.zeros(B * n, hq, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+            self.lse, self.lp, self.ent = torch.zeros(B * n, hq, device=DEV), torch.zeros(B * n, device=DEV), torch.zeros(B * n, device=DEV)
+            self.ids = torch.zeros(B * n, 7, dtype=torch.int32, device=DEV)
+
+        def step(self):
+            ctx.owl_kv_append_fp8(d, qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], None, rope, self.q, *self.cache, table, self.L, None)
+            ctx.owl_verify_attn_fp8(d, self.q, *self.cache, table, self.L, None, par, self.out, self.lse)
+            ctx.owl_token_logprobs(d, logits, tok, None, par, self.lp, self.ent, None, self.ids, None)
+            ctx.owl_kv_commit_fp8(d, *self.cache, table, self.L, None, alen, path)
+
+        def results(self):
+            return [self.q, self.out, self.lse, self.lp, self.ent, self.ids, self.L] + [x.view(torch.uint8) for x in self.cache]
+
+    a, b = State(), State()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        b.step()
+    for i in range(rounds):
+        a.step()
+        graph.replay()
+        for x, y in zip(a.results(), b.results()):
+            assert torch.equal(x, y)
+    assert a.L.tolist() == [x + rounds * y for x, y in zip(lens, (3, 4, 1))] and ctx.owl_get_status() == 0
+    del graph
+    ctx.close()
