@@ -529,6 +529,18 @@ __device__ __forceinline__ void wait_for_product(AuxFp8* aux, uint32_t seq) {
     __syncwarp();
     tc_fence_after();
 }
+// The softmax warps at a segment's end, its products awaited.  Whether the segment holds such drafted rows (they lie in the last two
+// tiles of a sequence at most) is read by the first softmax warp alone and left for all before they meet, because a hardware barrier
+// hangs on it: after a wait that gave up the converting and the producer warp may write the tiles' flags while others read them.
+__device__ __forceinline__ void meet_at_segment_end(AuxFp8* aux, const JointSegment& js) {
+    if (js.leader && (threadIdx.x & 31) == 0) {
+        const volatile uint8_t* nans = aux->nan_drafts;
+        const uint32_t T = (uint32_t)(js.g.tile1 - js.g.tile0), end = js.tile_base + T;
+        const bool some = nans[(end - 1u) % kNotes] || (T > 1u && nans[(end - 2u) % kNotes]);
+        const_cast<volatile int&>(aux->mark_drafts) = some && !*const_cast<volatile int*>(&aux->abort_flag);
+    }
+    meet_before_segment(aux, js.seg_no + 1, js.leader);
+}
 // S of the segment's tile i, in buffer `b`; `phases`: one bit per buffer, the phase of its barrier that comes next.
 __device__ __forceinline__ void wait_for_scores(AuxFp8* aux, uint32_t b, uint32_t& phases) {
     mbar_wait_certain(smem_u32(&aux->joint_s_full[b]), (phases >> b) & 1u, &aux->abort_flag);
@@ -668,7 +680,7 @@ __device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, u
     k->sum[s][wtid] = l;
     if (!idle) mbar_wait_certain(smem_u32(&aux->joint_o_done), done_phase & 1u, &aux->abort_flag);
     tc_fence_after();
-    meet_before_segment(aux, js.seg_no + 1, js.leader);      // both warpgroups done: all MMAs of the segment have completed
+    meet_at_segment_end(aux, js);          // both warpgroups done: all MMAs of the segment have completed
     const volatile Segment& again = aux->seg[js.seg_no % kSegs];
     const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
     const bool write_ok = !bad && !*const_cast<volatile int*>(&aux->abort_flag);
@@ -929,7 +941,7 @@ __device__ __forceinline__ void keys_segment(const AttnParams& p, AuxFp8* aux, u
     }
     mbar_wait_certain(smem_u32(&aux->joint_o_done), done_phase & 1u, &aux->abort_flag);
     tc_fence_after();
-    meet_before_segment(aux, js.seg_no + 1, js.leader);    // both warpgroups done: all MMAs of the segment have completed
+    meet_at_segment_end(aux, js);          // both warpgroups done: all MMAs of the segment have completed
     const volatile Segment& again = aux->seg[js.seg_no % kSegs];
     const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
     const bool write_ok = !bad && !*const_cast<volatile int*>(&aux->abort_flag);
@@ -1154,7 +1166,7 @@ __device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux,
     // ---- segment end: every product of this stream has completed
     mbar_wait_certain(smem_u32(&aux->o_done[s]), od_phase & 1u, abort_flag);
     tc_fence_after();
-    meet_before_segment(aux, js.seg_no + 1, js.leader);    // both streams done: all MMAs of the segment have completed
+    meet_at_segment_end(aux, js);          // both streams done: all MMAs of the segment have completed
     const volatile Segment& again = aux->seg[js.seg_no % kSegs];
     const bool bad = const_cast<volatile int&>(aux->seg_bad_tree) || again.bad_page;
     const bool write_ok = !bad && !*abort_flag;
@@ -1274,11 +1286,8 @@ __device__ __forceinline__ void softmax_loop_fp8(const AttnParams& p, AuxFp8* au
             ++joint_segs;
         }
         tc_fence_before();
-        const uint32_t T = (uint32_t)(g.tile1 - g.tile0);
-        tile_base += T;
-        // (drafted rows lie in the last two tiles of a sequence at most; alike in all threads)
-        const volatile uint8_t* nans = aux->nan_drafts;
-        if (nans[(tile_base - 1u) % kNotes] || (T > 1u && nans[(tile_base - 2u) % kNotes])) {
+        tile_base += (uint32_t)(g.tile1 - g.tile0);
+        if (const_cast<volatile int&>(aux->mark_drafts)) {      // alike in all threads; written again only after barrier 1 of the next segment
             named_barrier(1, 256);               // the results, which other threads have stored
             mark_nan_drafts(p, aux, seg_no);
         }

@@ -106,7 +106,10 @@ struct Aux {
     int seg_close;                   // no reader takes this segment or a later one (a wait for an announcement gave up)
     int seg_bad_tree;
     Segment seg[kSegs];
-    int sched_b0;
+    union {
+        int sched_b0;                // read before the roles begin
+        int mark_drafts;             // verify_attn_fp8.cuh: the segment that ended last has a drafted row of V with a NaN
+    };
     long long sched_tile_begin;
     long long scan_tiles[16];        // one place per warp of a CTA (16 in verify_attn_fp8.cuh)
     long long total_tiles;
