@@ -40,6 +40,7 @@
  *  - k_cache/v_cache  bf16 [num_pages, Hkv, page_size, D]; one (page, head) block is
  *                 page_size*D contiguous elements.  A contiguous cache is the same
  *                 layout with an identity block_table.
+ *                 q, out, k_cache and v_cache begin on 16-byte boundaries in every call that takes them.
  *  - block_table  int32 [B, max_pages_per_seq]: physical page of each logical page
  *  - ctx_lens     int32 [B]: committed context length L_b.  The K/V of drafted node i
  *                 of sequence b are already stored at logical position L_b + i, so the

@@ -390,6 +390,8 @@ int owl_destroy(owl_ctx* ctx) {
 
 static void launch_scan(owl_ctx* ctx, AcceptParams& p, cudaStream_t stream, bool early);
 static void launch_accept(owl_ctx* ctx, AcceptParams& p, cudaStream_t stream);
+// Rows of q, out and the caches are read and written in 16-byte pieces.
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Attention of a verify step.  `ap` non-null: the acceptance of the same step.  A small scan rides in the attention
 // kernel's spare warps, two launches for the whole step; a larger one (`own_scan`) is a kernel of its own between the
@@ -403,6 +405,7 @@ static int verify_attn_impl(owl_ctx* ctx, const owl_dims* d, const void* q, cons
     int rc = check_dims(d, true, false);
     if (rc != OWL_OK) return rc;
     if (!q || !k_cache || !v_cache || !block_table || !ctx_lens || !tree_parent || !out) return OWL_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return OWL_ERR_INVALID_ARG;
     if (!node_offsets && d->total_nodes % d->batch != 0) return OWL_ERR_INVALID_ARG;
     if (!ctx->part_o) return OWL_ERR_TOO_LARGE;
     const owl_dims& mx = ctx->max_dims;
@@ -692,6 +695,7 @@ static int commit_params(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v
         !(d->page_size == 16 || d->page_size == 32 || d->page_size == 64 || d->page_size == 128))
         return OWL_ERR_UNSUPPORTED;
     if (!k_cache || !v_cache || !block_table || !ctx_lens || !accept_len || !accept_path) return OWL_ERR_INVALID_ARG;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return OWL_ERR_INVALID_ARG;
     if (!node_offsets && d->total_nodes % d->batch != 0) return OWL_ERR_INVALID_ARG;
     p = CommitParams{};
     p.k_cache = static_cast<__nv_bfloat16*>(k_cache); p.v_cache = static_cast<__nv_bfloat16*>(v_cache);
@@ -724,8 +728,6 @@ int owl_kv_commit_fp8(owl_ctx* ctx, const owl_dims* d, void* k_cache, void* v_ca
     DeviceGuard guard(ctx->device);
     return launch_commit(ctx, kv_commit_fp8_kernel, p, p.base, stream_, "owl_kv_commit_fp8 launch");
 }
-
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // The append in all its forms: `page_exp` non-null for the 8-bit cache.
 static int kv_append_impl(owl_ctx* ctx, const owl_dims* d, int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
