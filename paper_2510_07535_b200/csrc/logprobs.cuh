@@ -303,7 +303,8 @@ static_assert(kMaxTop <= kScoreWarps * 8, "as many parts of the table as alterna
 template <typename T>
 __global__ void __launch_bounds__(kScoreWarps * 32) logprob_merge_kernel(const ScoreParams p) {
     constexpr int kThreads = kScoreWarps * 32, kPer = ScoreLoad<T>::kPer, kLoads = ScoreLoad<T>::kLoads;
-    __shared__ float s_max[kThreads / 4], s_edge, s_m, s_log_s;
+    __shared__ __align__(16) float s_max[kThreads / 4];
+    __shared__ float s_edge, s_m, s_log_s;
     __shared__ int s_groups[kScoreGroups], s_count[2];
     __shared__ unsigned long long s_keys[kScoreCandidates];
     asm volatile("griddepcontrol.wait;" ::: "memory");
