@@ -106,6 +106,7 @@ class OwlContext:
         if rc != OWL_OK:
             raise OwlError(rc, "owl_create")
         self._handle, self._dev = self._h.value, self.device.index      # as the native half takes them
+        self._max_rows = max_dims.total_nodes
 
     def close(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -202,6 +203,8 @@ class OwlContext:
             raise TypeError("top_ids and top_logprobs differ in their last dimension")
         if top == 0:
             top_ids = top_logprobs = None
+        if dims.total_nodes > self._max_rows:      # before the tensors are held against the rows
+            return self._done(-7, check, "owl_token_logprobs")
         rc = _native.token_logprobs(self._handle, self._dev, dims, top, logits, tokens, node_offsets, tree_parent, logprob, entropy, lse, top_ids,
                                     top_logprobs)
         return self._done(rc, check, "owl_token_logprobs")

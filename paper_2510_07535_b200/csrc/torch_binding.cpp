@@ -57,6 +57,21 @@ bool tensor_ptr(PyObject* o, const Spec& s, int device, void** out) {
     return true;
 }
 
+// A tensor (or None) has at least `count` elements.
+bool holds(PyObject* o, const char* name, int64_t count) {
+    if (o == Py_None || THPVariable_Unpack(o).numel() >= count) return true;
+    PyErr_Format(PyExc_TypeError, "%s: expected at least %lld elements, got %lld", name, (long long)count, (long long)THPVariable_Unpack(o).numel());
+    return false;
+}
+// The last dimension of a tensor (or None) with rows is `width`.
+bool rows_of(PyObject* o, const char* name, int64_t width) {
+    if (o == Py_None) return true;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.dim() < 2 || t.size(-1) == width) return true;
+    PyErr_Format(PyExc_TypeError, "%s: expected rows of %lld, got %lld", name, (long long)width, (long long)t.size(-1));
+    return false;
+}
+
 // `count` tensors from `args` on into pointers
 bool tensors(PyObject* const* args, const Spec* spec, size_t count, int device, void** ptr) {
     for (size_t i = 0; i < count; ++i)
@@ -280,6 +295,7 @@ PyObject* append_call(PyObject* const* args, Py_ssize_t nargs, bool fp8) {
         }
         rows = (int)t.size(0);
     }
+    if (!holds(args[6], "positions", d.total_nodes) || (q && !holds(args[8], "q_out", 128ll * d.total_nodes * d.num_q_heads))) return nullptr;
     auto i = [&](int n) { return static_cast<int32_t*>(p[n]); };
     const float* rope = static_cast<float*>(p[1]);
     void* stream = h.stream();
@@ -302,6 +318,8 @@ OWL_CALL(verify_attn_fp8) {
     const Spec s[] = {{"q", type}, {"k_cache", kE4m3}, {"v_cache", kE4m3}, {"page_exp", kI8}, {"block_table", kI32}, {"ctx_lens", kI32},
                       {"node_offsets", kI32}, {"tree_parent", kI32}, {"out", type}, {"lse", kF32}};
     if (!tensors(args + 3, s, 10, h.device, p)) return nullptr;
+    const int64_t rows = (int64_t)d.total_nodes * d.num_q_heads;
+    if (!holds(args[3], "q", 128 * rows) || !holds(args[11], "out", 128 * rows) || !holds(args[12], "lse", rows)) return nullptr;
     auto i = [&](int n) { return static_cast<int32_t*>(p[n]); };
     void* stream = h.stream();
     return unlocked([&] {
@@ -325,6 +343,14 @@ OWL_CALL(token_logprobs) {
     const Spec s[] = {{"logits", type}, {"tokens", kI32}, {"node_offsets", kI32}, {"tree_parent", kI32}, {"logprob", kF32}, {"entropy", kF32},
                       {"lse", kF32}, {"top_ids", kI32}, {"top_logprobs", kF32}};
     if (!tensors(args + 4, s, 9, h.device, p)) return nullptr;
+    // (the C call refuses a vocabulary or a number of alternatives below what there can be)
+    const int64_t rows = d.total_nodes, alternatives = top > 0 ? rows * top : 0;
+    if (d.vocab > 0 && (!rows_of(args[4], "logits", d.vocab) || !holds(args[4], "logits", rows * d.vocab))) return nullptr;
+    for (int n : {5, 7, 8, 9, 10})
+        if (!holds(args[n], s[n - 4].name, rows)) return nullptr;
+    if (!holds(args[6], "node_offsets", (int64_t)d.batch + 1) || !holds(args[11], "top_ids", alternatives) ||
+        !holds(args[12], "top_logprobs", alternatives))
+        return nullptr;
     auto i = [&](int n) { return static_cast<int32_t*>(p[n]); };
     auto f = [&](int n) { return static_cast<float*>(p[n]); };
     void* stream = h.stream();
