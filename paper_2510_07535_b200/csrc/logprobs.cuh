@@ -312,7 +312,8 @@ __global__ void __launch_bounds__(kScoreWarps * 32) logprob_merge_kernel(const S
     const int row = p.row0 + blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int per_chunk = (p.rounds + 1) * 32, groups = p.chunks * per_chunk;      // < 2^31: the table's row fits the context
     const float* maxima = p.maxima + (long long)blockIdx.x * groups;
-    // A thread holds its first 32 groups' maxima (8192 groups: all of a row of 200000 logits); the few beyond are read twice.
+    // A thread holds its first 32 groups' maxima: 8192 groups, which are 131072 logits in chunks of one round (64 groups each, half of them for
+    // the ragged ends) and more in longer ones; those beyond are read twice.
     constexpr int kHeld = 32;
     float held[kHeld];
     if (p.top > 0) {
