@@ -633,7 +633,8 @@ __device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, u
                 }
                 m = m_new;
             }
-            const float neg_m = m == -INFINITY ? 0.f : kWeightShift - m;
+            // (a row without a score above -inf so far: the first one there is goes beyond any threshold, so that it becomes the reference)
+            const float neg_m = m == -INFINITY ? 3.402823466e38f : kWeightShift - m;
             const uint64_t neg_m_x2 = pack_f32x2(neg_m, neg_m);
             uint64_t ex_a = 0ull, ex_b = 0ull;
             uint32_t buf[2][32];

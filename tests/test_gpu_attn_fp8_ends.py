@@ -1,10 +1,11 @@
-"""owl_verify_attn_fp8 where its number formats end: the smallest exponents of V, over the four ways in which a unit
-is worked on (32, 64, 124 and 240 packed rows)."""
+"""owl_verify_attn_fp8 where its number formats end: the smallest exponents of V, and scores that overflow, over the four
+ways in which a unit is worked on (32, 64, 124 and 240 packed rows)."""
 import numpy as np
 import pytest
 
+import oracle
 from paper_2510_07535_b200 import OwlContext, workloads as W
-from test_gpu_attn_fp8 import Case, run
+from test_gpu_attn_fp8 import Case, bits16, run
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +42,26 @@ def test_heads_of_small_values_alone(nodes, dtype):
     # the bound tells the values from nothing, in every head
     for h in range(5):
         assert (np.abs(want[:, 4 * h:4 * h + 4]) > 2 * tol[:, 4 * h:4 * h + 4]).mean() > 0.5, h
+
+
+@pytest.mark.parametrize("nodes", NODES)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("ctx", [[40000], [300, 9000, 17]])
+def test_a_first_tile_of_minus_infinity(nodes, dtype, ctx):
+    """Scores of the first tile's keys that overflow to minus infinity, and of 0 behind them.  The oracle has -128 for the former, of which e^-128
+    is no more than nothing either."""
+    c = Case(W.Spec("inf8", 8, 2, ctx, [("tree", nodes, 5)] * len(ctx), shuffle_pages=True, seed=nodes), dtype)
+    page = c.k8.shape[2]
+    c.exp[..., 0], c.k8[:] = 0, 0
+    for b, L in enumerate(ctx):
+        for pos in range(0, min(128, L - 1), page):
+            c.k8[c.wl.block_table[b, pos // page], :, :min(page, L - 1 - pos)] = oracle.e4m3_encode([1.0])[0]
+    c.q[:], c.scale = bits16(np.array([-1.0]), dtype)[0], 1.0
+    want, want_lse, tol, lse_tol = c.reference()
+    if dtype == "bf16":
+        c.q[:] = bits16(np.array([-2.0 ** 126]), dtype)[0]
+    else:
+        c.q[:], c.scale = bits16(np.array([-2.0 ** 10]), dtype)[0], 2.0 ** 120
+    out, lse = outputs(c)
+    assert (np.abs(lse - want_lse) <= lse_tol).all(), np.abs(lse - want_lse).max()
+    assert (np.abs(out - want) <= tol).all(), np.abs(out - want).max()
