@@ -81,7 +81,7 @@ __device__ __forceinline__ uint32_t joint_s(uint32_t buffer, uint32_t columns) {
 // What is known of a tile besides its bytes.  A place is written again eight tiles later: the producer is at most kRawTiles ahead of
 // Q K^T, and that at most three tiles ahead of the softmax warps, the last to look at it.
 struct TileNote {
-    float kscale[kTileKeys / 16];                // 2^e of K, for each 16 keys
+    float kscale[kTileKeys / 16];                // 2^(e + 24) of K, for each 16 keys (score_scale)
     int spans;                                   // low half: keys of the sequence in it (-1: no more tiles); high: of them, the context's
     int8_t vexp[kTileKeys / 16];                 // e of V
 };
@@ -173,7 +173,7 @@ __device__ __forceinline__ void producer_loop_fp8(const AttnParams& p, const CUt
             TileNote& note = aux->note[seq % kNotes];
             const int exp_kv = __shfl_sync(0xffffffffu, exps, in_block * ppt + ((lane * 16) >> p.page_shift));
             if (lane < kTileKeys / 16) {
-                note.kscale[lane] = exp2_int(max(kExpMin, min(kExpMax, (int)(int8_t)(exp_kv & 0xff))));
+                note.kscale[lane] = exp2_int(max(kExpMin, min(kExpMax, (int)(int8_t)(exp_kv & 0xff))) - kExpMin);
                 note.vexp[lane] = (int8_t)(exp_kv >> 8);
             }
             if (lane == 0) {
@@ -501,13 +501,20 @@ __device__ __forceinline__ float min_or_nan(float x, float y) {
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
     return r;
 }
-// What a row's sums of products are multiplied by, besides their page's 2^e.  Not below 2^-100, where all that is less makes scores that differ
-// by less than 2^-66: times 2^-24 it is no zero, and a score of -inf stays one.  (A NaN stays one, too.)
+// What a row's sums of products are multiplied by, besides their page's 2^(e + 24).  (The 2^24 keep the product of a row near the end of bf16's
+// range finite that the page's 2^e brings back.)  Not below 2^-124, where all that is less makes scores that differ by less than 2^-66: times
+// the smallest page's 1 it is no zero, and a score of -inf stays one.  (A NaN stays one, too.)
 __device__ __forceinline__ float score_scale(const AttnParams& p, float row_scale) {
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(p.sm_scale * 1.4426950408889634f * row_scale), "f"(exp2_int(-100)));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(p.sm_scale * (1.4426950408889634f * exp2_int(kExpMin)) * row_scale), "f"(exp2_int(-124)));
     return r;
 }
+// A score is rounded before its reference is subtracted, in the weights as in the reference itself.  A product fused with the difference is
+// not, and from references of this size on, whose neighbours lie further apart than 1, that makes the weight of the reference's own key
+// anything from nothing to infinity.  Joint units multiply by the row's number, rounded, and then by the page's power of two, which is
+// exact and may be fused.  Shared units fuse both while no row of the warp has a far reference (the joint units' form there: 4 x 64K of
+// fp16 320 instead of 314 us, 8 x 64K of bf16 with 64 query heads 550 instead of 532).
+constexpr float kFarReference = 16777216.f;
 // Meets `count` threads on hardware barrier `id`; true for all if it is for one.
 __device__ __forceinline__ bool any_of(int id, int count, bool mine) {
     uint32_t r;
@@ -608,7 +615,7 @@ __device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, u
                         float a = __uint_as_float(r[16 * hf]);
 #pragma unroll
                         for (int j = 1; j < 16; ++j) a = fmaxf(a, __uint_as_float(r[16 * hf + j]));
-                        mx = fmaxf(mx, a * (kscale[2 * c + hf] * scale2));
+                        mx = fmaxf(mx, a * scale2 * kscale[2 * c + hf]);
                     }
                 }
                 k->most[s][wtid] = mx;
@@ -635,7 +642,7 @@ __device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, u
             }
             // (a row without a score above -inf so far: the first one there is goes beyond any threshold, so that it becomes the reference)
             const float neg_m = m == -INFINITY ? 3.402823466e38f : kWeightShift - m;
-            const uint64_t neg_m_x2 = pack_f32x2(neg_m, neg_m);
+            const uint64_t neg_m_x2 = pack_f32x2(neg_m, neg_m), scale2_x2 = pack_f32x2(scale2, scale2);
             uint64_t ex_a = 0ull, ex_b = 0ull;
             uint32_t buf[2][32];
             tmem_ld32(tMine, buf[0]);
@@ -645,12 +652,13 @@ __device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, u
             tmem_loaded(buf[1]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const float s0 = kscale[2 * c] * scale2, s1 = kscale[2 * c + 1] * scale2;
-                const uint64_t s0_x2 = pack_f32x2(s0, s0), s1_x2 = pack_f32x2(s1, s1);
+                const float k0 = kscale[2 * c], k1 = kscale[2 * c + 1];
+                const uint64_t k0_x2 = pack_f32x2(k0, k0), k1_x2 = pack_f32x2(k1, k1);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     float x0, x1;
-                    const uint64_t xx = fma_f32x2(pack_f32x2(__uint_as_float(buf[c][2 * j]), __uint_as_float(buf[c][2 * j + 1])), j < 8 ? s0_x2 : s1_x2, neg_m_x2);
+                    const uint64_t product = mul_f32x2(pack_f32x2(__uint_as_float(buf[c][2 * j]), __uint_as_float(buf[c][2 * j + 1])), scale2_x2);
+                    const uint64_t xx = fma_f32x2(product, j < 8 ? k0_x2 : k1_x2, neg_m_x2);
                     unpack_f32x2(xx, x0, x1);
                     const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
                     pk[c * 16 + j] = pack2_16bit<true>(p0, p1);
@@ -1049,6 +1057,7 @@ __device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux,
     const unsigned long long anc_row = rr < g.M ? aux->anc[row_node(p, rr)] : 0ull;
     const float scale2 = score_scale(p, aux->row_scale[rr]);
     float m = -INFINITY, l = 0.f;
+    bool near = false;                   // all of the warp's rows have a reference, and none a far one
     for (int i = 0; i < T; ++i) {
         const int t = g.tile0 + i;
         const uint32_t seq = js.tile_base + (uint32_t)i;
@@ -1082,10 +1091,10 @@ __device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux,
             tmem_wait_st();
         }
         bool done = false, force = false;
-        if (i > 0 && !__any_sync(0xffffffffu, m == -INFINITY)) done = weigh_tile(tS, kscale, scale2, m, l, force);
+        if (near) done = weigh_tile(tS, kscale, scale2, m, l, force);
         if (!done) {
             // The long way: the tile's maximum first, then the weights; twice over tensor memory and rolled, because
-            // it runs on a segment's first tile and after a jump of the maximum only.
+            // it runs on a segment's first tile, after a jump of the maximum and on rows of no or a far reference only.
             float mx = -INFINITY;
 #pragma unroll 1
             for (int c4 = 0; c4 < 4; ++c4) {
@@ -1125,6 +1134,7 @@ __device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux,
                 }
                 m = m_new;
             }
+            near = !__any_sync(0xffffffffu, fabsf(m) >= kFarReference);
             const float neg_m = (m == -INFINITY) ? 0.f : kWeightShift - m;
             float sum = 0.f;
 #pragma unroll 1
@@ -1138,7 +1148,8 @@ __device__ __forceinline__ void shared_segment(const AttnParams& p, AuxFp8* aux,
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const float sc = kscale[2 * c4 + (j >> 3)] * scale2;
-                    const float p0 = fast_exp2(fmaf(__uint_as_float(sv[2 * j]), sc, neg_m)), p1 = fast_exp2(fmaf(__uint_as_float(sv[2 * j + 1]), sc, neg_m));
+                    const float p0 = fast_exp2(__fadd_rn(__fmul_rn(__uint_as_float(sv[2 * j]), sc), neg_m));
+                    const float p1 = fast_exp2(__fadd_rn(__fmul_rn(__uint_as_float(sv[2 * j + 1]), sc), neg_m));
                     pk[j] = pack2_16bit<true>(p0, p1);
                     x_a += p0; x_b += p1;
                 }

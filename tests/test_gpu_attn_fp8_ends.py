@@ -1,7 +1,8 @@
-"""owl_verify_attn_fp8 where its number formats end: the smallest exponents of V, and scores that overflow, over the four
-ways in which a unit is worked on (32, 64, 124 and 240 packed rows)."""
+"""owl_verify_attn_fp8 where its number formats end: the smallest exponents of V, and scores as large as the formats allow, over the four ways
+in which a unit is worked on (32, 64, 124 and 240 packed rows)."""
 import numpy as np
 import pytest
+import torch
 
 import oracle
 from paper_2510_07535_b200 import OwlContext, workloads as W
@@ -65,3 +66,34 @@ def test_a_first_tile_of_minus_infinity(nodes, dtype, ctx):
     out, lse = outputs(c)
     assert (np.abs(lse - want_lse) <= lse_tol).all(), np.abs(lse - want_lse).max()
     assert (np.abs(out - want) <= tol).all(), np.abs(out - want).max()
+
+
+@pytest.mark.parametrize("nodes", NODES)
+@pytest.mark.parametrize("dtype,exp,size", [(t, 7, s) for t in ("bf16", "f16") for s in (0, 6, 10, 14)] + [("bf16", 7, 100), ("bf16", -24, 120)])
+def test_scores_far_beyond_their_whole_numbers(nodes, dtype, exp, size):
+    """Scores of 2^20 to 2^34, whose fp32 neighbours lie up to 2^11 apart, and near the end of fp32's range: one key has all the weight, or
+    two in tiles apart share it."""
+    c = Case(W.Spec("large8", 8, 2, [9000, 50], [("tree", nodes, 5), ("chain", 3)], shuffle_pages=True, seed=nodes + size), dtype)
+    rng = np.random.default_rng(nodes + size)
+    page = c.k8.shape[2]
+    c.exp[..., 0] = exp
+    c.k8[:] = rng.integers(0, 0x7D, c.k8.shape[:3])[..., None]               # up to 384, alike in all of a row's elements
+    top = [[(5, 1505), (4021, 8021)], [(48, 48), (0, 0)]]                    # of each sequence and KV head: 448
+    where = lambda b, h, i: (c.wl.block_table[b, top[b][h][i] // page], h, top[b][h][i] % page)  # noqa: E731
+    for b in range(2):
+        for h in range(2):
+            c.k8[where(b, h, 0)] = c.k8[where(b, h, 1)] = 0x7E
+    x = (1 + rng.integers(0, 128, c.q.shape[:2]) / 128) * 2.0 ** size         # eight significant bits
+    c.q[:] = bits16(np.broadcast_to(x[..., None], c.q.shape), dtype)
+    c.scale = 128 ** -0.5
+    out, lse = outputs(c)
+    v = oracle.cache8_values(c.v8, c.exp, 1)
+    n = np.diff(c.wl.node_offsets)
+    both = [np.concatenate([np.stack([v[where(b, hq // 4, i)] for hq in range(8)])[None].repeat(n[b], 0) for b in range(2)]) for i in range(2)]
+    want, size = (both[0] + both[1]) / 2, (np.abs(both[0]) + np.abs(both[1])) / 2
+    # a weight of its own rounding to fp16 over its sum, the merge's factors, and the output's half step
+    tol = size * (2.0 ** -11 + 2.0 ** -18) + np.abs(want) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -11) + 2.0 ** -24
+    assert (np.abs(out - want) <= tol).all(), (np.abs(out - want) / tol).max()
+    # 128 products cut off at an ulp each, then the scale and the reference
+    score = 128 * x * 448 * 2.0 ** exp * np.float64(np.float32(c.scale))
+    assert (np.abs(lse - score) <= score * (128 + 8) * 2.0 ** -23 + 1e-5).all(), (np.abs(lse - score) / score).max()
