@@ -95,8 +95,10 @@ typedef struct owl_dims {
 } owl_dims;
 
 /* Create a context on `device` with workspace for any call whose dims do not exceed
- * `max_dims` (batch, total_nodes, max_nodes, heads).  Allocates device memory once;
- * later calls allocate nothing.  Host-synchronous. */
+ * `max_dims` (batch, total_nodes, max_nodes, heads, vocab).  Allocates device memory once;
+ * later calls allocate nothing.  With heads it holds partials of the attention, with a vocabulary
+ * (max_dims->vocab > 0) the acceptance's keys and, for owl_token_logprobs, up to 16.5 MB and 8 bytes per
+ * row (more only where one row of that vocabulary needs it).  Host-synchronous. */
 int owl_create(owl_ctx** ctx, int device, const owl_dims* max_dims);
 
 /* Free the context's device memory.  The caller must have synchronised every stream
@@ -113,6 +115,8 @@ int owl_destroy(owl_ctx* ctx);
  *   lse[n,hq]    = ln sum_k exp(sm_scale * q[n,hq].K_k)
  * Computed by split-KV kernels: per KV chunk an online-softmax pass on the tensor
  * cores producing fp32 partials in the context's workspace, then an LSE merge.
+ * Scores sm_scale * q.K_k are meant to stay below 2^24 in magnitude: a row with one of 2^27 (fp16) or 2^30
+ * (bf16) may come out as NaN.  (owl_verify_attn_fp8 takes any that fp32 holds.)
  * Asynchronous on `stream`.  `lse` may be NULL.
  */
 int owl_verify_attn(owl_ctx* ctx, const owl_dims* dims, const void* q, const void* k_cache,
@@ -319,7 +323,9 @@ int owl_kv_commit_fp8(owl_ctx* ctx, const owl_dims* dims, void* k_cache, void* v
  * top_* are.  NaN and -inf logits have probability 0 and are no alternatives (missing ones: id -1, -inf).  A row
  * without anything else has lse -inf, entropy 0 and every log probability -inf; a row with +inf has lse +inf, entropy NaN
  * and log probability -inf for finite logits, NaN for infinite ones.  A malformed offset or parent sets
- * OWL_ERR_BAD_TREE and leaves that node's logprob unwritten.  Asynchronous on `stream`; results do not depend on timing.
+ * OWL_ERR_BAD_TREE and leaves that node's logprob unwritten.  dims as for the acceptance, so at most 64 rows to a sequence
+ * (max_nodes <= 64, max_nodes * batch >= total_nodes); with tree_parent NULL the division into sequences has no meaning and a prompt's rows
+ * may be declared as any that fits.  Asynchronous on `stream`; results do not depend on timing.
  */
 int owl_token_logprobs(owl_ctx* ctx, const owl_dims* dims, int32_t dtype, const void* logits, const int32_t* tokens,
                        const int32_t* node_offsets, const int32_t* tree_parent, int32_t top, float* logprob, float* entropy,

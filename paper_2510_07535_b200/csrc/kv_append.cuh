@@ -15,7 +15,8 @@
 //
 // Bound by the rows' bytes for a prompt, by one chain of dependent loads (offsets, length, table, row) for a draft: 8191 tokens to 8
 // bits with 32 + 16 heads take 38.5 us (189 MB, 4.9 TB/s, 75 % of the copy bandwidth), four prompts of 2047 in fp16 63.6 us (340 MB,
-// 5.3 TB/s, 81 %), a chain of 8 or 16 trees of 32 about 3 and 5 us on the device and 9.3 us from call to call, which is the host's.
+// 5.3 TB/s, 81 %; to 8 bits a barrier stands between a head's loads and its stores, and 16 bytes spill under the 64 registers that
+// 1024 threads leave), a chain of 8 or 16 trees of 32 about 3 and 5 us on the device and 9.3 us from call to call, which is the host's.
 #pragma once
 
 #include "fp8_block.cuh"

@@ -7,9 +7,9 @@
 //   logprob_merge_kernel  a CTA per row joins the chunks:  lse = m + ln s,  entropy = ln s - t / s,  scores a token, and finds
 //                         the alternatives: of 64 maxima over parts of the table the top-th largest is not above the top-th
 //                         largest logit, so the groups of 32 whose maximum reaches it hold all of them, some tens of groups.
-// 256 rows of 128256 fp32 logits with 20 alternatives take 30.2 us (131 MB, 4.3 TB/s, 66 % of the copy bandwidth); 8 rows 9.3 us, the
-// latency of two launches.
-// Bound by the logits' bytes: per element a maximum, a subtraction, a product, a clamp, an ex2 and two sums.  (A sorted list per warp in the
+// 256 rows of 128256 fp32 logits with 20 alternatives take 30.0 us (131 MB, 4.4 TB/s, 67 % of the copy bandwidth), 23.9 of them the scan; of bf16
+// or fp16 ones 24.6 and 19.4 (66 MB, 2.7 TB/s, 41 %); 8 rows 9.9 to 10.4 us, the latency of two launches.
+// fp32 logits are bound by their bytes, 16-bit ones, which are half of them, by the work per logit: per element a maximum, a subtraction, a product, a clamp, an ex2 and two sums.  (A sorted list per warp in the
 // scan instead of the table: 256 rows of 128256 fp32 logits 42.8 us with 20 alternatives and 23.9 without, 8 rows 13.9 and 2.7.)
 #pragma once
 
@@ -65,7 +65,7 @@ __device__ __forceinline__ void join_sums(float& m, float& s, float& t, float m2
     m = mm;
 }
 
-// One lane's 32 logits of a round (kWide: 4-byte elements, four per load; else eight).
+// One lane's 32 logits of a round, 16 bytes to a load: four logits of 4 bytes or eight of 2.
 template <typename T> struct ScoreLoad {
     static constexpr int kPer = 16 / (int)sizeof(T), kLoads = 32 / kPer;
     uint4 u[kLoads];
@@ -451,7 +451,9 @@ __global__ void __launch_bounds__(kScoreWarps * 32) logprob_merge_kernel(const S
 }
 
 // Logits per item, a multiple of a round: the size that ends first when the resident warps take the items in turn, an item costing what
-// `kItemCost` more logits would (its first round waits for memory and finds the list's limit, its end joins the lanes' sums).
+// `kItemCost` more logits would (its first round waits for memory, its end joins the lanes' sums).  Rows of 128256 logits, us, at 0 / 350 / 700 /
+// 1400 / 2800: 32 rows of fp32 16.0 / 12.5 / 12.5 / 12.5 / 12.5, 256 30.3 / 29.7 / 29.8 / 29.8 / 29.8, of bf16 26.0 / 24.6 / 24.7 / 24.6 /
+// 24.6, 960 of bf16 89.9 / 89.9 / 90.0 / 72.8 / 72.8.
 // At most `most` items; where no size keeps to that, the largest one (the caller then takes the rows in several turns).
 inline int score_chunk(long long rows, int vocab, int sms, long long most) {
     constexpr long long kItemCost = 700;

@@ -12,10 +12,17 @@
 //
 // Two e4m3 products of 128x128x32 take the time of one fp16 pair, so the tensor pipe does the work of the 16-bit caches' pass; HBM brings half
 // of its bytes, and shared memory carries per tile 32 KB from TMA, 64 for Q K^T, 16 + 32 for the conversion and 32 for P V.  (A
-// form that turned K into fp16 as well moved 224 KB, kept the ring half as deep, and took 453 instead of 283 us on 16 chains of 8 at 4K to 64K.)
-// What bounds it: from some 16 long sequences on the board's 1000 W.  16 chains run at 1.9 GHz and 4.0 TB/s, 62 % of the copy
-// bandwidth; 16 trees of 32, 128 rows a unit, at 1.6 GHz and 850 TFLOP/s of Q K^T and P V (and weights of 16 ex2 a clock: 1024
-// of a tile's 1700 clocks); one tree of 32 at 32K (31 us) and a chain at 2K (13 us) are set-up, first copies and the merge.
+// form that turned K into fp16 as well moved 224 KB, kept the ring half as deep, and took 453 us on 16 chains of 8 at 4K to 64K, where
+// this one takes 283 to 305.)
+// What bounds it: no unit of an SM alone.  A tile of a chain takes some 2300 clocks, of which HBM needs 1370 at the copy bandwidth, the softmax
+// warps work 970 (and wait 510 for the product two tiles back) and the converting warps 1310 (and wait 670 for their slot and 500 for V): the
+// ring of these is what a tile takes; 16 chains run at 4.0 TB/s, 62 % of the copy bandwidth.  16 trees of 32, 128 rows a unit, take 1700 clocks a
+// tile, 1024 of them exponentials at 16 ex2 a clock.  One tree of 32 at 32K (31 to 33 us) is 14 such tiles a CTA and 10 us of start
+// and merge, and some 13 us that are not accounted for; a chain at 2K (13 us) is set-up, first copies and the merge.
+// Back to back the long cases also meet the board's 1000 W.  One GPU, a pass alone / back to back and its SM clock: 16 chains 305 / 302 us
+// at 1.85 GHz, 16 mixed 338 / 387 at 1.78, 16 trees of 32 350 / 399 at 1.53, 4 x 64K of fp16 342 / 362 at 1.63 (of 1.965 GHz).
+// The instances for wide units spill: 28 to 112 bytes of stores and 32 to 340 of loads at 176 registers for the softmax warps, those for
+// narrow ones 0 to 4 and 0 to 44.
 //
 // 16 warps:
 //   warp 0        TMA producer: one box per (page, head) of K and of V into a ring of tiles of 2 x 16 KB; leaves each tile's note
@@ -27,13 +34,13 @@
 // verify_attn_umma.cuh.
 // Other units ("joint"): both softmax warpgroups work on each tile, one O, and three S, so that Q K^T runs up to three tiles ahead and no
 // softmax waits for the products of the tile before.  (With two streams that took the tiles by turns, each waiting for its own
-// P V and Q K^T, a 128-row tile took 2100 clocks: 16 chains of 64-row units 411 us instead of 312.)
+// P V and Q K^T, a 128-row tile took 2100 clocks: 16 chains of 64-row units 411 us, now 312 to 360.)
 //   65 to 128 rows: rows on the lanes, each warpgroup weighs half of a tile's keys; the two share the rows' references.
 //   up to 64 rows:  keys on the lanes.  The products are turned round,
 //       S^T = K Q^T   [128 keys x pieces * rows], the pieces' columns added up in registers,
 //       O^T += V^T P  [128 channels x rows],      P [keys x rows] through shared memory,
 //     so that a unit of 32 rows does not pay for 128 of them: the products take an eighth and a quarter of the multipliers (and of the
-//     power, which is what sets the clock here), a softmax thread has one key and half of the rows, every lane is in use, and sums
+//     power, which sets the clock where calls follow each other), a softmax thread has one key and half of the rows, every lane is in use, and sums
 //     over keys are kept per thread until the segment's end.
 #pragma once
 
@@ -254,7 +261,8 @@ __device__ __forceinline__ void convert_loop(const AttnParams& p, AuxFp8* aux, u
             // A tile that holds drafted rows, or ends.  Rows past the sequence's end may hold anything, and their weight of 0 does not make a
             // NaN harmless; nor does it that of a drafted row in the rows of Q that do not see its node: such NaNs are left out, and those that
             // do see it get them at the segment's end (mark_nan_drafts).  Apart from the other tiles, and short: with this looked at in
-            // every tile 16 mixed sequences of 4K to 64K took 468 us, unrolled by two in the loop's middle 360, like this 340.
+            // every tile 16 mixed sequences of 4K to 64K took 468 us, unrolled by two in the loop's middle 360, like this 340 on the same GPU
+            // (from one GPU to the next 312 to 390).
 #pragma unroll 1
             for (int j = 0; j < 8; ++j) {
                 const int key = (4 * warp + (j >> 1)) * 8 + key7;
