@@ -116,7 +116,7 @@ int owl_destroy(owl_ctx* ctx);
  * Computed by split-KV kernels: per KV chunk an online-softmax pass on the tensor
  * cores producing fp32 partials in the context's workspace, then an LSE merge.
  * Scores sm_scale * q.K_k are meant to stay below 2^24 in magnitude: a row with one of 2^27 (fp16) or 2^30
- * (bf16) may come out as NaN.  (owl_verify_attn_fp8 takes any that fp32 holds.)
+ * (bf16) may come out as NaN.  (owl_verify_attn_fp8 takes any that fp32 holds, to fp32's spacing there.)
  * Asynchronous on `stream`.  `lse` may be NULL.
  */
 int owl_verify_attn(owl_ctx* ctx, const owl_dims* dims, const void* q, const void* k_cache,

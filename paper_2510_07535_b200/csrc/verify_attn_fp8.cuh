@@ -495,6 +495,7 @@ __device__ __forceinline__ void load_q_fp8(const AttnParams& p, const Segment& g
 // key has all the weight, and two conversions and an addition per pair of keys less (8 trees of 32 at 64K, 64 query heads: 647 -> 592 us).
 constexpr float kWeightShift = 7.f;
 constexpr float kWeightLimit = 32768.f;          // 2^(8 + 7)
+constexpr float kNoReference = 3.402823466e38f;  // in the place of 7 - m: takes any score above -inf beyond the limit
 // log-sum-exp of a row from its reference and its sum of shifted weights (a NaN sum stays one)
 __device__ __forceinline__ float lse_of_sum(float m, float sum) {
     return sum > 0.f ? (m - kWeightShift + __log2f(sum)) * 0.6931471805599453f : sum == 0.f ? -INFINITY : sum;
@@ -649,7 +650,7 @@ __device__ __forceinline__ void rows_segment(const AttnParams& p, AuxFp8* aux, u
                 m = m_new;
             }
             // (a row without a score above -inf so far: the first one there is goes beyond any threshold, so that it becomes the reference)
-            const float neg_m = m == -INFINITY ? 3.402823466e38f : kWeightShift - m;
+            const float neg_m = m == -INFINITY ? kNoReference : kWeightShift - m;
             const uint64_t neg_m_x2 = pack_f32x2(neg_m, neg_m), scale2_x2 = pack_f32x2(scale2, scale2);
             uint64_t ex_a = 0ull, ex_b = 0ull;
             uint32_t buf[2][32];
@@ -756,7 +757,7 @@ struct KeysStream {
             const int row = row0() + wtid;
             // rows beyond M: weights of 0; others: any score at all is above the threshold until the first reference is there
             k->scale[row] = row < g.M ? score_scale(p, aux->row_scale[row]) : 0.f;
-            k->bias[row] = row < g.M ? 1e30f : -INFINITY;
+            k->bias[row] = row < g.M ? kNoReference : -INFINITY;
             k->m[row] = -INFINITY;
         }
 #pragma unroll

@@ -69,6 +69,30 @@ def test_a_first_tile_of_minus_infinity(nodes, dtype, ctx):
 
 
 @pytest.mark.parametrize("nodes", NODES)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_first_tile_of_minus_infinity_before_scores_near_it(nodes, dtype):
+    """The first tile's scores overflow, all others are alike, -2^109 or -2^113.  (A log-sum-exp of that size in 32 bits says nothing of how many
+    keys are in it, so what the pieces of a sequence weigh against each other is open: all keys but the first tile's have the same value.)"""
+    c = Case(W.Spec("near8", 8, 2, [60000, 300], [("tree", nodes, 5)] * 2, shuffle_pages=True, seed=nodes), dtype)
+    page, n = c.k8.shape[2], 2 * nodes
+    first = c.wl.block_table[:, :128 // page]
+    c.k8[:], c.exp[..., 0] = oracle.e4m3_encode([1.0])[0], -24
+    c.exp[first, :, 0] = 0
+    v = oracle.cache8_values(c.v8, c.exp, 1)[0, :, 0]                # [KV heads, 128]
+    c.v8[:], c.exp[..., 1] = c.v8[:1, :, :1], c.exp[:1, :, 1]
+    c.v8[first] ^= 0x80
+    if dtype == "bf16":
+        c.q[:], c.scale = bits16(np.array([-2.0 ** 126]), dtype)[0], 1.0
+    else:
+        c.q[:], c.scale = bits16(np.array([-2.0 ** 10]), dtype)[0], 2.0 ** 120
+    out, lse = outputs(c)
+    assert (np.abs(lse / -2.0 ** (109 if dtype == "bf16" else 113) - 1) <= 2.0 ** -20).all(), lse
+    # equal weights, rounded to fp16 alike, over their sum; the output's half step
+    want = np.repeat(v, 4, 0)[None].repeat(n, 0)
+    assert (np.abs(out - want) <= np.abs(want) * (2.0 ** -11 + 2.0 ** -16 + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -11))).all(), np.abs(out - want).max()
+
+
+@pytest.mark.parametrize("nodes", NODES)
 @pytest.mark.parametrize("dtype,exp,size", [(t, 7, s) for t in ("bf16", "f16") for s in (0, 6, 10, 14)] + [("bf16", 7, 100), ("bf16", -24, 120)])
 def test_scores_far_beyond_their_whole_numbers(nodes, dtype, exp, size):
     """Scores of 2^20 to 2^34, whose fp32 neighbours lie up to 2^11 apart, and near the end of fp32's range: one key has all the weight, or
