@@ -17,8 +17,8 @@
 // What bounds it: no unit of an SM alone.  A tile of a chain takes some 2300 clocks, of which HBM needs 1370 at the copy bandwidth, the softmax
 // warps work 970 (and wait 510 for the product two tiles back) and the converting warps 1310 (and wait 670 for their slot and 500 for V): the
 // ring of these is what a tile takes; 16 chains run at 4.0 TB/s, 62 % of the copy bandwidth.  16 trees of 32, 128 rows a unit, take 1700 clocks a
-// tile, 1024 of them exponentials at 16 ex2 a clock.  One tree of 32 at 32K (31 to 33 us) is 14 such tiles a CTA and 10 us of start
-// and merge, and some 13 us that are not accounted for; a chain at 2K (13 us) is set-up, first copies and the merge.
+// tile, 1024 of them exponentials at 16 ex2 a clock.  One tree of 32 at 32K (31 to 33 us) is 14 such tiles a CTA, 12 us, 10 us of
+// start and merge, and some 10 us that are not accounted for; a chain at 2K (13 us) is set-up, first copies and the merge.
 // Back to back the long cases also meet the board's 1000 W.  One GPU, a pass alone / back to back and its SM clock: 16 chains 305 / 302 us
 // at 1.85 GHz, 16 mixed 338 / 387 at 1.78, 16 trees of 32 350 / 399 at 1.53, 4 x 64K of fp16 342 / 362 at 1.63 (of 1.965 GHz).
 // The instances for wide units spill: 28 to 112 bytes of stores and 32 to 340 of loads at 176 registers for the softmax warps, those for
